@@ -218,6 +218,149 @@ bra_status bra_backward(const bra_problem* p, const void* Q, const void* K, cons
                         float* d_lce_w, float* d_lce_b,
                         void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * What stands around the attention of a block.  The rules at the top hold here too (device pointers,
+ * 16-byte aligned, asynchronous on `stream`, errors found on the host return before any launch).
+ * Tensors are [B, N, channels] by tokens (a feature map's H x W tokens are N = H * W of them); a
+ * stride counts ELEMENTS from one token to the next, 0 stands for dense rows, images follow one
+ * another N * stride elements apart, so a tensor may be a slice of channels of a wider one.
+ * ------------------------------------------------------------------------------------------------ */
+
+/* Channels of a head that make a pair: neighbours (2i, 2i+1), or (i, i + n/2) of a block of n. */
+typedef enum bra_rope_layout { BRA_ROPE_INTERLEAVED = 0, BRA_ROPE_HALF = 1 } bra_rope_layout;
+
+/*
+ * Rotary positions.  The first rot_dim channels of every head are rotated, the others copied.  With axes
+ * = 2 the rotated channels are two blocks of n = rot_dim / 2, the first turned by a token's first
+ * coordinate (its row), the second by its second (its column); with axes = 1 they are one block.
+ * Pair i of a block turns by the angle coordinate * freq[i], formed in 64 bits:
+ *   (u, v) -> magnitude * (u cos - v sin, u sin + v cos).
+ */
+typedef struct bra_rope_problem {
+    int32_t B, N;             /* images (or sequences), tokens of each */
+    int32_t heads, kv_heads;  /* heads of Q and of K (kv_heads 0: there is no K) */
+    int32_t head_dim;
+    int32_t rot_dim;          /* a multiple of 2 * axes, at most head_dim */
+    int32_t layout;           /* bra_rope_layout */
+    int32_t axes;             /* 1 or 2 */
+    int32_t width;            /* axes = 2 without positions: token t is at row t / width, column t % width */
+    int32_t first;            /* axes = 1 without positions: token t is at first + t (>= 0) */
+    int32_t dtype;            /* bra_dtype */
+    float   magnitude;        /* factor on rotated channels; <= 0 selects 1 */
+    int64_t q_stride, k_stride;
+} bra_rope_problem;
+
+/* How frequencies are stretched for contexts longer than those a network was trained on. */
+typedef enum bra_rope_scaling {
+    BRA_ROPE_PLAIN = 0,   /* f_i = base^(-2i/n) */
+    BRA_ROPE_LINEAR = 1,  /* f_i / factor */
+    BRA_ROPE_BASE = 2,    /* base * factor^(n/(n-2)) in the place of base: the slowest pair is stretched by factor (n > 2) */
+    BRA_ROPE_PARTS = 3    /* pairs with r = original_length * f_i / 2 pi >= high turns keep f_i, those with r <= low get
+                             f_i / factor, those between a mean of the two, linear in r */
+} bra_rope_scaling;
+
+/* Host only: the rot_dim / axes / 2 frequencies of a block, into the HOST array freq. */
+bra_status bra_rope_frequencies(int32_t rot_dim, int32_t axes, double base, int32_t scaling, double factor,
+                                double original_length, double low, double high, double* freq);
+
+/*
+ * Rotates Q and K (K NULL iff kv_heads is 0) in one launch.
+ *   positions in   int32 [B, N, axes], or NULL: those that the problem implies
+ *   freq      in   double [rot_dim / axes / 2], on the device
+ *   inverse   in   nonzero: by the negative angle.  That is the transpose, so it is also the gradient:
+ *                  dQ = bra_rope(inverse) of the gradient of Qo.
+ *   Qo, Ko    out  laid out like Q, K; each may be the very same tensor (in place)
+ */
+bra_status bra_rope(const bra_rope_problem* p, const void* Q, const void* K, const int32_t* positions,
+                    const double* freq, int32_t inverse, void* Qo, void* Ko, void* stream);
+
+/*
+ * Cross attention: the queries of a map attend to an encoder's states.  Query head h reads key / value
+ * head h / (heads / kv_heads).  Key j of image b is visible iff j < key_len[b] (where key_len is given;
+ * below 0 counts as 0) and key_mask[b, j] != 0 (where key_mask is given).  What stands in hidden keys and
+ * values, infinities and NaN included, reaches no output.  A query that sees no key (or whose scores
+ * are all -inf) has O = 0, lse = -inf and adds nothing to any gradient.
+ */
+typedef struct bra_cross_problem {
+    int32_t B, Nq, Nk;        /* images, queries and keys of each */
+    int32_t heads, kv_heads;  /* kv_heads divides heads */
+    int32_t head_dim;         /* 16, 32, 64 or 128 */
+    int32_t dtype;            /* bra_dtype */
+    float   scale;            /* softmax scale; <= 0 selects 1/sqrt(head_dim) */
+    int64_t q_stride, k_stride, v_stride;   /* multiples of 16 bytes */
+} bra_cross_problem;
+
+/* Scratch size in bytes of both calls (0 if p is invalid).  Host only.  Like the routed attention's, this scratch has to be
+ * zero before its first use and is left ready for the next one; calls that share it must be ordered on one stream. */
+size_t bra_cross_workspace_bytes(const bra_cross_problem* p);
+
+/*
+ * O = softmax(scale * Q K^T over visible keys) V.
+ *   Q        in   [B, Nq, heads, head_dim], q_stride
+ *   K, V     in   [B, Nk, kv_heads, head_dim], k_stride and v_stride
+ *   key_len  in   int32 [B]; may be NULL.   key_mask  in  uint8 [B, Nk]; may be NULL
+ *   O        out  [B, Nq, heads, head_dim], dense
+ *   lse      out  fp32 [B, heads, Nq], natural log of the softmax denominator of the scaled scores; may be NULL
+ */
+bra_status bra_cross_attend(const bra_cross_problem* p, const void* Q, const void* K, const void* V,
+                            const int32_t* key_len, const uint8_t* key_mask, void* O, float* lse,
+                            void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Its gradients, from O and lse of bra_cross_attend on the same inputs and dO (dense, like O).
+ *   dQ, dK, dV  out  laid out like Q, K, V (same strides); hidden keys get zeros.  dK and dV of a key head are
+ *                    the sums over its query heads.  The order of every sum is fixed.
+ */
+bra_status bra_cross_backward(const bra_cross_problem* p, const void* Q, const void* K, const void* V,
+                              const int32_t* key_len, const uint8_t* key_mask, const void* O, const float* lse,
+                              const void* dO, void* dQ, void* dK, void* dV,
+                              void* ws, size_t ws_bytes, void* stream);
+
+typedef enum bra_norm { BRA_NORM_NONE = 0, BRA_NORM_RMS = 1, BRA_NORM_LAYER = 2 } bra_norm;
+typedef enum bra_gate { BRA_GATE_NONE = 0, BRA_GATE_CHANNEL = 1, BRA_GATE_IMAGE = 2 } bra_gate;
+
+/*
+ * The norms on both sides of a block's end, fused with its gate and residual scale:
+ *   y' = post(y) * post_w + post_b       (post = BRA_NORM_NONE: y' = y)
+ *   h  = alpha * x + gate * y'           the residual stream behind the block
+ *   n  = pre(h) * w + b                  what the next block reads (pre = BRA_NORM_NONE: no n)
+ * with rms(v) = v / sqrt(mean(v^2) + eps) and layer(v) = (v - mean v) / sqrt(var v + eps) over the C channels of
+ * a token.  Everything between x, y and the outputs is fp32; n is made from h before its rounding.
+ */
+typedef struct bra_norm_problem {
+    int32_t B, N, C;          /* images, tokens of each, channels (at most 8192) */
+    int32_t pre, post;        /* bra_norm */
+    int32_t gate;             /* bra_gate: no gate, fp32 [C], fp32 [B, C] */
+    int32_t per_image;        /* nonzero: w and b are fp32 [B, C] (modulated by a condition), else [C] */
+    int32_t dtype;            /* bra_dtype of x, y, h, n and their gradients */
+    float   eps, alpha;
+} bra_norm_problem;
+
+/* Scratch size in bytes of bra_residual_norm_backward (0 if p is invalid).  Host only.  It needs no initial value. */
+size_t bra_norm_workspace_bytes(const bra_norm_problem* p);
+
+/*
+ *   x     in   [B, N, C]
+ *   y     in   [B, N, C], the block's output; NULL: h = alpha * x (the first norm of a network; gate and post must be 0)
+ *   gate  in   NULL iff p->gate is BRA_GATE_NONE.   post_w, post_b, w, b  in  each may be NULL (ones, zeros)
+ *   h     out  [B, N, C]; may be NULL, may be x or y.   n  out  [B, N, C]; NULL iff p->pre is BRA_NORM_NONE
+ */
+bra_status bra_residual_norm(const bra_norm_problem* p, const void* x, const void* y, const float* gate,
+                             const float* post_w, const float* post_b, const float* w, const float* b,
+                             void* h, void* n, void* stream);
+
+/*
+ * Gradients.  dh: of h from what follows in the stream, may be NULL (zeros).  dn: of n, NULL iff p->pre is
+ * BRA_NORM_NONE.  dx [B, N, C]; dy [B, N, C], NULL iff y is; the others are fp32 in the shapes of their
+ * inputs, each may be NULL where it is not wanted.  The forward pass is made again from x and y, so nothing
+ * else has to be kept; the order of every sum is fixed.
+ */
+bra_status bra_residual_norm_backward(const bra_norm_problem* p, const void* x, const void* y, const float* gate,
+                                      const float* post_w, const float* post_b, const float* w,
+                                      const void* dh, const void* dn, void* dx, void* dy, float* d_gate,
+                                      float* d_post_w, float* d_post_b, float* d_w, float* d_b,
+                                      void* ws, size_t ws_bytes, void* stream);
+
 /*
  * Synchronises `stream`, then returns and clears the first device-detected
  * error recorded in ws (BRA_OK, BRA_ERR_INDEX, BRA_ERR_TIMEOUT, or BRA_ERR_CUDA

@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_float, c_int32, c_size_t, c_void_p
+from ctypes import c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 
 _LIB = None
 _TORCH = None            # torch, once it has shown a CUDA device
@@ -37,6 +37,35 @@ class BraProblem(ctypes.Structure):
     @property
     def heads_i(self):
         return 1 if self.shared_routing else self.heads
+
+
+class BraRopeProblem(ctypes.Structure):
+    """Mirror of `bra_rope_problem`."""
+
+    _fields_ = [
+        ("B", c_int32), ("N", c_int32), ("heads", c_int32), ("kv_heads", c_int32), ("head_dim", c_int32),
+        ("rot_dim", c_int32), ("layout", c_int32), ("axes", c_int32), ("width", c_int32), ("first", c_int32),
+        ("dtype", c_int32), ("magnitude", c_float), ("q_stride", c_int64), ("k_stride", c_int64),
+    ]
+
+
+class BraCrossProblem(ctypes.Structure):
+    """Mirror of `bra_cross_problem`."""
+
+    _fields_ = [
+        ("B", c_int32), ("Nq", c_int32), ("Nk", c_int32), ("heads", c_int32), ("kv_heads", c_int32),
+        ("head_dim", c_int32), ("dtype", c_int32), ("scale", c_float),
+        ("q_stride", c_int64), ("k_stride", c_int64), ("v_stride", c_int64),
+    ]
+
+
+class BraNormProblem(ctypes.Structure):
+    """Mirror of `bra_norm_problem`."""
+
+    _fields_ = [
+        ("B", c_int32), ("N", c_int32), ("C", c_int32), ("pre", c_int32), ("post", c_int32), ("gate", c_int32),
+        ("per_image", c_int32), ("dtype", c_int32), ("eps", c_float), ("alpha", c_float),
+    ]
 
 
 class BraError(RuntimeError):
@@ -77,6 +106,24 @@ def load_library():
     lib.bra_forward.argtypes = [P, v, v, v, v, v, v, v, v, v, c_size_t, v]
     lib.bra_backward.restype = c_int32
     lib.bra_backward.argtypes = [P] + [v] * 12 + [v, c_size_t, v]
+    lib.bra_rope_frequencies.restype = c_int32
+    lib.bra_rope_frequencies.argtypes = [c_int32, c_int32, c_double, c_int32, c_double, c_double, c_double, c_double, v]
+    lib.bra_rope.restype = c_int32
+    lib.bra_rope.argtypes = [ctypes.POINTER(BraRopeProblem), v, v, v, v, c_int32, v, v, v]
+    PC = ctypes.POINTER(BraCrossProblem)
+    lib.bra_cross_workspace_bytes.restype = c_size_t
+    lib.bra_cross_workspace_bytes.argtypes = [PC]
+    lib.bra_cross_attend.restype = c_int32
+    lib.bra_cross_attend.argtypes = [PC] + [v] * 8 + [c_size_t, v]
+    lib.bra_cross_backward.restype = c_int32
+    lib.bra_cross_backward.argtypes = [PC] + [v] * 12 + [c_size_t, v]
+    PN = ctypes.POINTER(BraNormProblem)
+    lib.bra_norm_workspace_bytes.restype = c_size_t
+    lib.bra_norm_workspace_bytes.argtypes = [PN]
+    lib.bra_residual_norm.restype = c_int32
+    lib.bra_residual_norm.argtypes = [PN] + [v] * 10
+    lib.bra_residual_norm_backward.restype = c_int32
+    lib.bra_residual_norm_backward.argtypes = [PN] + [v] * 16 + [c_size_t, v]
     lib.bra_device_status.restype = c_int32
     lib.bra_device_status.argtypes = [v, v]
     lib.bra_last_launch_count.restype = c_int32
@@ -268,3 +315,219 @@ def bra_backward(p, Q, K, V, index, lce_w, lse, dO, dQ=None, dK=None, dV=None, d
 def bra_device_status(ws, stream=None) -> int:
     """Synchronise the stream and return (and clear) the first device-detected error in ws."""
     return int(load_library().bra_device_status(_ptr(ws), _stream(stream)))
+
+
+# ---------------------------------------------------------------- what stands around the attention of a block
+# These calls take tensors of a program's own making (slices of fused projections, masks, positions), so what a wrong one would
+# make the kernels read is checked here: element type, number of elements, order in memory, device.
+_DTYPES = {"f32": F32, "bf16": BF16, F32: F32, BF16: BF16}
+
+
+def _tensor(t, name, where, dtype, numel, device, optional=False, tokens=None):
+    """Address of a dense tensor of `numel` elements on the current device; with tokens = (images, tokens, channels, stride) of a
+    [images, tokens, channels] view whose tokens lie `stride` elements apart."""
+    if t is None:
+        if optional:
+            return None
+        raise BraError(1, f"{where}: {name}")
+    if t.dtype is not dtype:
+        raise BraError(4, f"{where}: {name} is {t.dtype}, not {dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{where}: {name} is on {t.device}, the current device is cuda:{device}")
+    if t.numel() != numel:
+        raise BraError(2, f"{where}: {name} has {t.numel()} elements, not {numel}")
+    if tokens is not None:
+        B, N, C, stride = tokens
+        if stride != C:
+            if t.dim() != 3 or tuple(t.shape) != (B, N, C) or (C > 1 and t.stride(2) != 1) or (N > 1 and t.stride(1) != stride) or \
+                    (B > 1 and t.stride(0) != N * stride):
+                raise BraError(2, f"{where}: {name} is not a [{B}, {N}, {C}] view with {stride} elements from token to token")
+            return t.data_ptr()
+    if not t.is_contiguous():
+        raise BraError(2, f"{where}: {name} is not contiguous")
+    return t.data_ptr()
+
+
+def _current_device():
+    torch = _torch()
+    get = getattr(torch._C, "_cuda_getDevice", None)
+    return get() if get else torch.cuda.current_device()
+
+
+def _like(t, tokens):
+    """A new tensor laid out as `t` (a slice of channels of a wider tensor stays one)."""
+    torch = _torch()
+    B, N, C, stride = tokens
+    if stride == C:
+        return torch.empty_like(t)
+    return torch.empty(B, N, stride, dtype=t.dtype, device=t.device)[..., :C]
+
+
+def _scratch(nbytes, where, device):
+    if nbytes == 0:
+        raise BraError(2, where)
+    return _torch().zeros(nbytes, dtype=_torch().uint8, device=device)
+
+
+def make_rope_problem(B, N, heads, head_dim, kv_heads=None, rot_dim=None, layout="interleaved", axes=1, width=0, first=0,
+                      dtype="bf16", magnitude=1.0, q_stride=0, k_stride=0) -> BraRopeProblem:
+    return BraRopeProblem(B, N, heads, heads if kv_heads is None else kv_heads, head_dim,
+                          head_dim if rot_dim is None else rot_dim, {"interleaved": 0, "half": 1}[layout], axes, width, first,
+                          _DTYPES[dtype], float(magnitude), q_stride, k_stride)
+
+
+def rope_frequencies(rot_dim, axes=1, base=10000.0, scaling="none", factor=1.0, original_length=0.0, low=1.0, high=32.0,
+                     device="cuda"):
+    """bra_rope_frequencies, on the device: fp64 [rot_dim / axes / 2].  Made once and kept with the layer."""
+    torch = _torch()
+    out = torch.empty(max(0, rot_dim // axes // 2), dtype=torch.float64)
+    _check(load_library().bra_rope_frequencies(rot_dim, axes, float(base), {"none": 0, "linear": 1, "base": 2, "parts": 3}[scaling],
+                                               float(factor), float(original_length), float(low), float(high), _ptr(out)),
+           "bra_rope_frequencies")
+    return out.to(device)
+
+
+def bra_rope(p, Q, K, freq, positions=None, Qo=None, Ko=None, inverse=False, stream=None):
+    """bra_rope: Q, K -> (Qo, Ko).  Pass Q and K as Qo and Ko to rotate in place; inverse=True is the gradient's rotation."""
+    torch = _torch()
+    dev, t, where = _current_device(), _tdtype(p), "bra_rope"
+    q = (p.B, p.N, p.heads * p.head_dim, p.q_stride or p.heads * p.head_dim)
+    k = (p.B, p.N, p.kv_heads * p.head_dim, p.k_stride or p.kv_heads * p.head_dim)
+    n = p.B * p.N
+    q_at = _tensor(Q, "Q", where, t, n * q[2], dev, tokens=q)
+    k_at = _tensor(K, "K", where, t, n * k[2], dev, optional=not p.kv_heads, tokens=k)
+    f_at = _tensor(freq, "freq", where, torch.float64, p.rot_dim // p.axes // 2 if p.axes else 0, dev)
+    at = _tensor(positions, "positions", where, torch.int32, n * p.axes, dev, optional=True)
+    Qo = _like(Q, q) if Qo is None else Qo
+    Ko = _like(K, k) if Ko is None and K is not None else Ko
+    _check(load_library().bra_rope(ctypes.byref(p), q_at, k_at, at, f_at, int(bool(inverse)),
+                                   _tensor(Qo, "Qo", where, t, n * q[2], dev, tokens=q),
+                                   _tensor(Ko, "Ko", where, t, n * k[2], dev, optional=not p.kv_heads, tokens=k), _stream(stream)), where)
+    return Qo, Ko
+
+
+def make_cross_problem(B, Nq, Nk, heads, head_dim, kv_heads=None, dtype="bf16", scale=0.0, q_stride=0, k_stride=0,
+                       v_stride=0) -> BraCrossProblem:
+    return BraCrossProblem(B, Nq, Nk, heads, heads if kv_heads is None else kv_heads, head_dim, _DTYPES[dtype], float(scale),
+                           q_stride, k_stride, v_stride)
+
+
+def cross_workspace_bytes(p: BraCrossProblem) -> int:
+    return int(load_library().bra_cross_workspace_bytes(ctypes.byref(p)))
+
+
+def cross_workspace(p: BraCrossProblem, device="cuda"):
+    """Zero-filled scratch tensor of bra_cross_workspace_bytes(p) bytes."""
+    return _scratch(cross_workspace_bytes(p), "bra_cross_workspace_bytes", device)
+
+
+def _cross_tokens(p):
+    C, Ck = p.heads * p.head_dim, p.kv_heads * p.head_dim
+    return (p.B, p.Nq, C, p.q_stride or C), (p.B, p.Nk, Ck, p.k_stride or Ck), (p.B, p.Nk, Ck, p.v_stride or Ck), (p.B, p.Nq, C, C)
+
+
+def _cross_mask(p, key_len, key_mask, where, dev):
+    torch = _torch()
+    len_at = _tensor(key_len, "key_len", where, torch.int32, p.B, dev, optional=True)
+    if key_mask is not None and key_mask.dtype is torch.bool:
+        return len_at, _tensor(key_mask, "key_mask", where, torch.bool, p.B * p.Nk, dev)
+    return len_at, _tensor(key_mask, "key_mask", where, torch.uint8, p.B * p.Nk, dev, optional=True)
+
+
+def bra_cross_attend(p, Q, K, V, key_len=None, key_mask=None, O=None, lse=None, ws=None, stream=None, want_lse=True):
+    """bra_cross_attend: Q, K, V -> (O, lse).  key_len int32 [B], key_mask bool or uint8 [B, Nk]."""
+    torch = _torch()
+    dev, t, where = _current_device(), _tdtype(p), "bra_cross_attend"
+    q, k, v, o = _cross_tokens(p)
+    nq, nk = p.B * p.Nq * q[2], p.B * p.Nk * k[2]
+    ins = [_tensor(Q, "Q", where, t, nq, dev, tokens=q), _tensor(K, "K", where, t, nk, dev, tokens=k),
+           _tensor(V, "V", where, t, nk, dev, tokens=v), *_cross_mask(p, key_len, key_mask, where, dev)]
+    ws = cross_workspace(p, Q.device) if ws is None else ws
+    O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device) if O is None else O
+    if lse is None and want_lse:
+        lse = torch.empty(p.B, p.heads, p.Nq, dtype=torch.float32, device=Q.device)
+    _check(load_library().bra_cross_attend(ctypes.byref(p), *ins, _tensor(O, "O", where, t, nq, dev),
+                                           _tensor(lse, "lse", where, torch.float32, p.B * p.heads * p.Nq, dev, optional=True),
+                                           _tensor(ws, "ws", where, torch.uint8, ws.numel(), dev), ws.numel(), _stream(stream)), where)
+    return O, lse
+
+
+def bra_cross_backward(p, Q, K, V, O, lse, dO, key_len=None, key_mask=None, dQ=None, dK=None, dV=None, ws=None, stream=None):
+    """bra_cross_backward: -> (dQ, dK, dV)."""
+    torch = _torch()
+    dev, t, where = _current_device(), _tdtype(p), "bra_cross_backward"
+    q, k, v, o = _cross_tokens(p)
+    nq, nk = p.B * p.Nq * q[2], p.B * p.Nk * k[2]
+    ins = [_tensor(Q, "Q", where, t, nq, dev, tokens=q), _tensor(K, "K", where, t, nk, dev, tokens=k),
+           _tensor(V, "V", where, t, nk, dev, tokens=v), *_cross_mask(p, key_len, key_mask, where, dev),
+           _tensor(O, "O", where, t, nq, dev), _tensor(lse, "lse", where, torch.float32, p.B * p.heads * p.Nq, dev),
+           _tensor(dO, "dO", where, t, nq, dev)]
+    ws = cross_workspace(p, Q.device) if ws is None else ws
+    dQ = _like(Q, q) if dQ is None else dQ
+    dK = _like(K, k) if dK is None else dK
+    dV = _like(V, v) if dV is None else dV
+    _check(load_library().bra_cross_backward(ctypes.byref(p), *ins, _tensor(dQ, "dQ", where, t, nq, dev, tokens=q),
+                                             _tensor(dK, "dK", where, t, nk, dev, tokens=k),
+                                             _tensor(dV, "dV", where, t, nk, dev, tokens=v),
+                                             _tensor(ws, "ws", where, torch.uint8, ws.numel(), dev), ws.numel(), _stream(stream)), where)
+    return dQ, dK, dV
+
+
+_NORMS, _GATES = {"none": 0, "rms": 1, "layer": 2}, {"none": 0, "channel": 1, "image": 2}
+
+
+def make_norm_problem(B, N, C, pre="layer", post="none", gate="none", per_image=False, alpha=1.0, eps=1e-6,
+                      dtype="bf16") -> BraNormProblem:
+    return BraNormProblem(B, N, C, _NORMS[pre], _NORMS[post], _GATES[gate], int(bool(per_image)), _DTYPES[dtype], float(eps), float(alpha))
+
+
+def norm_workspace_bytes(p: BraNormProblem) -> int:
+    return int(load_library().bra_norm_workspace_bytes(ctypes.byref(p)))
+
+
+def norm_workspace(p: BraNormProblem, device="cuda"):
+    """Scratch tensor of bra_norm_workspace_bytes(p) bytes (for the gradients)."""
+    return _scratch(norm_workspace_bytes(p), "bra_norm_workspace_bytes", device)
+
+
+def _norm_weights(p, gate, post_w, post_b, w, b, where, dev):
+    f32 = _torch().float32
+    affine = p.C * (p.B if p.per_image else 1)
+    return [_tensor(gate, "gate", where, f32, p.C * (p.B if p.gate == 2 else 1), dev, optional=p.gate == 0),
+            _tensor(post_w, "post_w", where, f32, p.C, dev, optional=True), _tensor(post_b, "post_b", where, f32, p.C, dev, optional=True),
+            _tensor(w, "w", where, f32, affine, dev, optional=True), _tensor(b, "b", where, f32, affine, dev, optional=True)]
+
+
+def bra_residual_norm(p, x, y=None, gate=None, post_w=None, post_b=None, w=None, b=None, h=None, n=None, stream=None, want_h=True):
+    """bra_residual_norm: x, y -> (h, n): the residual stream behind the block, and what the next block reads."""
+    torch = _torch()
+    dev, t, where, size = _current_device(), _tdtype(p), "bra_residual_norm", p.B * p.N * p.C
+    ins = [_tensor(x, "x", where, t, size, dev), _tensor(y, "y", where, t, size, dev, optional=True),
+           *_norm_weights(p, gate, post_w, post_b, w, b, where, dev)]
+    h = torch.empty_like(x) if h is None and want_h else h
+    n = torch.empty_like(x) if n is None and p.pre else n
+    _check(load_library().bra_residual_norm(ctypes.byref(p), *ins, _tensor(h, "h", where, t, size, dev, optional=True),
+                                            _tensor(n, "n", where, t, size, dev, optional=True), _stream(stream)), where)
+    return h, n
+
+
+def bra_residual_norm_backward(p, x, y, dh, dn, gate=None, post_w=None, post_b=None, w=None, b=None, dx=None, dy=None, ws=None,
+                               stream=None):
+    """bra_residual_norm_backward: -> {"dx", "dy", and of the weights that are given "dgate", "d_post_w", "d_post_b", "dw", "db"}."""
+    torch = _torch()
+    dev, t, where, size = _current_device(), _tdtype(p), "bra_residual_norm_backward", p.B * p.N * p.C
+    weights = _norm_weights(p, gate, post_w, post_b, w, b, where, dev)
+    ins = [_tensor(x, "x", where, t, size, dev), _tensor(y, "y", where, t, size, dev, optional=True), *weights[:4],
+           _tensor(dh, "dh", where, t, size, dev, optional=True), _tensor(dn, "dn", where, t, size, dev, optional=True)]
+    ws = norm_workspace(p, x.device) if ws is None else ws
+    out = {"dx": torch.empty_like(x) if dx is None else dx}
+    if y is not None:
+        out["dy"] = torch.empty_like(y) if dy is None else dy
+    for name, weight in (("dgate", gate), ("d_post_w", post_w), ("d_post_b", post_b), ("dw", w), ("db", b)):
+        if weight is not None:
+            out[name] = torch.empty_like(weight)
+    _check(load_library().bra_residual_norm_backward(
+        ctypes.byref(p), *ins, _tensor(out["dx"], "dx", where, t, size, dev), _tensor(out.get("dy"), "dy", where, t, size, dev, optional=True),
+        *(_ptr(out.get(name)) for name in ("dgate", "d_post_w", "d_post_b", "dw", "db")),
+        _tensor(ws, "ws", where, torch.uint8, ws.numel(), dev), ws.numel(), _stream(stream)), where)
+    return out

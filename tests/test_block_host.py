@@ -1,0 +1,198 @@
+"""Rotary positions, cross attention and residual norms at the C boundary without a GPU: refusals, frequencies, scratch sizes."""
+import ctypes
+import math
+
+import pytest
+
+A = 0x10000  # a fake, aligned, never dereferenced device address
+NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, UNSUPPORTED = 1, 2, 4, 5, 6, 7
+
+
+@pytest.fixture(scope="module")
+def bra():
+    import paper_2303_08810_b200 as pkg
+    from paper_2303_08810_b200 import build
+    build.build_library()
+    pkg.load_library()
+    return pkg
+
+
+def with_fields(p, kw):
+    for k, v in kw.items():
+        setattr(p, k, v)
+    return p
+
+
+# ---------------------------------------------------------------- rotary positions
+def rope(bra, kw=None, Q=A, K=A, positions=None, freq=A, Qo=A, Ko=A):
+    p = with_fields(bra.make_rope_problem(2, 5, 4, 32, kv_heads=2), kw or {})
+    return bra.load_library().bra_rope(ctypes.byref(p), Q, K, positions, freq, 0, Qo, Ko, None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(B=0), SHAPE), (dict(N=-1), SHAPE), (dict(heads=0), SHAPE), (dict(kv_heads=-1), SHAPE), (dict(head_dim=0), SHAPE),
+    (dict(rot_dim=0), SHAPE), (dict(rot_dim=33), SHAPE), (dict(rot_dim=34), SHAPE), (dict(rot_dim=31), SHAPE),
+    (dict(axes=0), SHAPE), (dict(axes=3), SHAPE), (dict(axes=2), SHAPE), (dict(axes=2, rot_dim=30, width=5), SHAPE),
+    (dict(first=-1), SHAPE), (dict(first=2 ** 31 - 3), SHAPE), (dict(q_stride=127), SHAPE), (dict(k_stride=63), SHAPE),
+    (dict(B=2 ** 30, N=2 ** 30), SHAPE), (dict(dtype=5), DTYPE), (dict(layout=2), UNSUPPORTED),
+    (dict(head_dim=2 ** 24, rot_dim=32), SHAPE),
+])
+def test_rope_refuses_bad_problems(bra, kw, code):
+    assert rope(bra, kw) == code
+    assert bra.last_launch_count() == 0
+
+
+def test_rope_refuses_bad_pointers(bra):
+    assert rope(bra, Q=None) == NULL and rope(bra, K=None) == NULL and rope(bra, Ko=None) == NULL and rope(bra, freq=None) == NULL
+    assert rope(bra, dict(kv_heads=0)) == NULL                      # K given, but no heads of it
+    assert rope(bra, Q=A + 8) == ALIGN and rope(bra, Ko=A + 2) == ALIGN and rope(bra, freq=A + 4) == ALIGN
+    assert rope(bra, positions=A + 2) == ALIGN
+    assert bra.load_library().bra_rope(None, A, A, None, A, 0, A, A, None) == NULL
+
+
+def frequencies(bra, n, axes=1, base=10000.0, scaling=0, factor=1.0, length=0.0, low=1.0, high=32.0):
+    out = (ctypes.c_double * max(1, n // axes // 2))()
+    code = bra.load_library().bra_rope_frequencies(n, axes, base, scaling, factor, length, low, high, out)
+    return code, list(out)
+
+
+def test_rope_frequencies(bra):
+    code, plain = frequencies(bra, 64)
+    assert code == 0
+    assert plain == pytest.approx([10000 ** (-i / 32) for i in range(32)], rel=1e-14)
+    assert frequencies(bra, 64, axes=2)[1] == pytest.approx(plain[::2], rel=1e-14)
+    assert frequencies(bra, 64, scaling=1, factor=4.0)[1] == pytest.approx([f / 4 for f in plain], rel=1e-14)
+    changed = frequencies(bra, 64, scaling=2, factor=8.0)[1]
+    assert changed[0] == 1.0 and changed[-1] == pytest.approx(plain[-1] / 8, rel=1e-12)
+    parts = frequencies(bra, 64, scaling=3, factor=8.0, length=4096.0)[1]
+    for f, g in zip(plain, parts):
+        turns = 4096 * f / (2 * math.pi)
+        if turns >= 32:
+            assert g == f
+        elif turns <= 1:
+            assert g == pytest.approx(f / 8, rel=1e-14)
+        else:
+            assert f / 8 < g < f
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(n=0), SHAPE), (dict(n=7), SHAPE), (dict(n=6, axes=2), SHAPE), (dict(n=8, axes=3), SHAPE), (dict(n=8, base=0.0), SHAPE),
+    (dict(n=8, base=math.nan), SHAPE), (dict(n=8, scaling=4), UNSUPPORTED), (dict(n=8, scaling=1, factor=0.0), SHAPE),
+    (dict(n=2, scaling=2, factor=2.0), SHAPE), (dict(n=8, scaling=3, factor=2.0), SHAPE),
+    (dict(n=8, scaling=3, factor=2.0, length=10.0, low=2.0, high=2.0), SHAPE),
+])
+def test_rope_frequencies_refuses(bra, kw, code):
+    assert frequencies(bra, **kw)[0] == code
+
+
+# ---------------------------------------------------------------- cross attention
+def cross(bra, kw=None, ws=A, ws_bytes=1 << 40, mask=None, length=None, back=False, **at):
+    p = with_fields(bra.make_cross_problem(2, 40, 24, 4, 32, kv_heads=2), kw or {})
+    get = lambda n: at.get(n, A)                                                                # noqa: E731
+    lib = bra.load_library()
+    if back:
+        return lib.bra_cross_backward(ctypes.byref(p), get("Q"), get("K"), get("V"), length, mask, get("O"), get("lse"), get("dO"),
+                                      get("dQ"), get("dK"), get("dV"), ws, ws_bytes, None)
+    return lib.bra_cross_attend(ctypes.byref(p), get("Q"), get("K"), get("V"), length, mask, get("O"), get("lse"), ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("kw,code", [
+    (dict(B=0), SHAPE), (dict(Nq=0), SHAPE), (dict(Nk=0), SHAPE), (dict(heads=0), SHAPE), (dict(kv_heads=0), SHAPE),
+    (dict(kv_heads=3), SHAPE), (dict(kv_heads=8), SHAPE), (dict(head_dim=-32), SHAPE), (dict(dtype=2), DTYPE),
+    (dict(head_dim=24), UNSUPPORTED), (dict(head_dim=256), UNSUPPORTED), (dict(q_stride=120), SHAPE), (dict(k_stride=60), SHAPE),
+    (dict(v_stride=8), SHAPE), (dict(q_stride=130), ALIGN), (dict(k_stride=68), ALIGN), (dict(v_stride=65), ALIGN),
+    (dict(Nq=2 ** 30, heads=4), SHAPE), (dict(B=2 ** 20, Nk=2 ** 25), SHAPE), (dict(k_stride=2 ** 40), SHAPE),
+])
+def test_cross_refuses_bad_problems(bra, kw, code, back):
+    assert cross(bra, kw, back=back) == code
+    assert bra.last_launch_count() == 0
+    p = with_fields(bra.make_cross_problem(2, 40, 24, 4, 32, kv_heads=2), kw)
+    assert bra.cross_workspace_bytes(p) == 0
+
+
+def test_cross_refuses_bad_pointers(bra):
+    for n in ("Q", "K", "V", "O"):
+        assert cross(bra, **{n: None}) == NULL and cross(bra, **{n: A + 8}) == ALIGN
+    for n in ("Q", "K", "V", "O", "dO", "dQ", "dK", "dV"):
+        assert cross(bra, back=True, **{n: None}) == NULL and cross(bra, back=True, **{n: A + 4}) == ALIGN
+    assert cross(bra, back=True, lse=None) == NULL and cross(bra, lse=A + 2) == ALIGN and cross(bra, length=A + 1) == ALIGN
+    for back in (False, True):
+        assert cross(bra, ws=None, back=back) == NULL and cross(bra, ws=A + 128, back=back) == ALIGN
+        need = bra.cross_workspace_bytes(bra.make_cross_problem(2, 40, 24, 4, 32, kv_heads=2))
+        assert cross(bra, ws_bytes=need - 1, back=back) == WORKSPACE
+        assert cross(bra, dict(Nk=2 ** 19 + 1), mask=A, back=back) == UNSUPPORTED      # bits of a mask are held in shared memory
+
+
+def test_cross_scratch_covers_split_sums(bra):
+    """Where output tiles are few the sums are split, and the scratch holds every part."""
+    few = bra.make_cross_problem(1, 1, 8192, 8, 64, kv_heads=1)
+    many = bra.make_cross_problem(64, 512, 8192, 8, 64, kv_heads=1)
+    assert bra.cross_workspace_bytes(few) > 8192 * 4                # more than counters and statistics
+    stats = 64 * 4096 * 8
+    assert stats < bra.cross_workspace_bytes(many) <= stats + 16384 + 4096
+
+
+# ---------------------------------------------------------------- residual norms
+def norm(bra, kw=None, back=False, ws=A, ws_bytes=1 << 40, **at):
+    p = with_fields(bra.make_norm_problem(2, 5, 64, pre="layer", post="rms", gate="channel"), kw or {})
+    B = A + (1 << 20)
+    base = dict(x=A, y=A, gate=A, post_w=A, post_b=None, w=A, b=A, h=B, n=2 * B, dh=A, dn=A, dx=3 * B, dy=4 * B, dg=B, dpw=B, dpb=None, dw=B, db=B)
+    base.update(at)
+    g = base.get
+    lib = bra.load_library()
+    if back:
+        return lib.bra_residual_norm_backward(ctypes.byref(p), g("x"), g("y"), g("gate"), g("post_w"), g("post_b"), g("w"), g("dh"), g("dn"),
+                                              g("dx"), g("dy"), g("dg"), g("dpw"), g("dpb"), g("dw"), g("db"), ws, ws_bytes, None)
+    return lib.bra_residual_norm(ctypes.byref(p), g("x"), g("y"), g("gate"), g("post_w"), g("post_b"), g("w"), g("b"), g("h"), g("n"), None)
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("kw,code", [
+    (dict(B=0), SHAPE), (dict(N=0), SHAPE), (dict(C=0), SHAPE), (dict(eps=-1.0), SHAPE), (dict(eps=math.nan), SHAPE),
+    (dict(B=2 ** 20, N=2 ** 20), SHAPE), (dict(dtype=9), DTYPE), (dict(pre=3), UNSUPPORTED), (dict(post=-1), UNSUPPORTED),
+    (dict(gate=3), UNSUPPORTED), (dict(C=8200), UNSUPPORTED),
+])
+def test_norm_refuses_bad_problems(bra, kw, code, back):
+    assert norm(bra, kw, back=back) == code
+    assert bra.last_launch_count() == 0
+    p = with_fields(bra.make_norm_problem(2, 5, 64), kw)
+    assert bra.norm_workspace_bytes(p) == 0
+
+
+def test_norm_refuses_bad_pointers(bra):
+    assert norm(bra, x=None) == NULL and norm(bra, n=None) == NULL and norm(bra, gate=None) == NULL
+    assert norm(bra, y=None) == NULL                                 # a gate and a norm of nothing
+    assert norm(bra, dict(pre=0)) == NULL                            # n is given, but there is no norm
+    assert norm(bra, dict(pre=0), n=None, h=None) == NULL            # nothing to write
+    assert norm(bra, dict(gate=0)) == NULL
+    assert norm(bra, n=A) == UNSUPPORTED                             # n over x
+    for n in ("x", "y", "gate", "post_w", "post_b", "w", "b", "h", "n"):
+        assert norm(bra, **{n: A + 4}) == ALIGN
+    assert norm(bra, back=True, dx=None) == NULL and norm(bra, back=True, dn=None) == NULL and norm(bra, back=True, dy=None) == NULL
+    assert norm(bra, dict(pre=0), back=True, dn=None, dh=None, dw=None, db=None) == NULL
+    assert norm(bra, dict(post=0), back=True) == UNSUPPORTED         # a gradient of weights that do not exist
+    assert norm(bra, dict(gate=0), back=True, gate=None) == UNSUPPORTED
+    assert norm(bra, dict(pre=0), back=True, dn=None) == UNSUPPORTED
+    B = A + (1 << 20)
+    assert norm(bra, back=True, dy=3 * B) == UNSUPPORTED and norm(bra, back=True, dx=A) == UNSUPPORTED
+    assert norm(bra, back=True, ws=None) == NULL and norm(bra, back=True, ws=A + 16) == ALIGN
+    need = bra.norm_workspace_bytes(bra.make_norm_problem(2, 5, 64, pre="layer", post="rms", gate="channel"))
+    assert norm(bra, back=True, ws_bytes=need - 1) == WORKSPACE
+
+
+def test_problem_structures_match_the_header(bra):
+    """Sizes as a C compiler lays the structures out."""
+    import os
+    import subprocess
+    import tempfile
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = '#include <stdio.h>\n#include "bra.h"\nint main(void){printf("%zu %zu %zu %zu",sizeof(bra_problem),sizeof(bra_rope_problem),' \
+           'sizeof(bra_cross_problem),sizeof(bra_norm_problem));return 0;}\n'
+    with tempfile.TemporaryDirectory() as d:
+        src, exe = os.path.join(d, "s.c"), os.path.join(d, "s")
+        with open(src, "w") as f:
+            f.write(code)
+        subprocess.run(["gcc", "-I", os.path.join(root, "include"), "-o", exe, src], check=True)
+        sizes = [int(v) for v in subprocess.run([exe], capture_output=True, text=True, check=True).stdout.split()]
+    assert sizes == [ctypes.sizeof(t) for t in (bra.BraProblem, bra.BraRopeProblem, bra.BraCrossProblem, bra.BraNormProblem)]
