@@ -15,6 +15,7 @@
 // every time.  Run c of the rows meets image b at most once, and walking runs and images together raises c or b by at least one from
 // one meeting to the next, so c + b numbers the meetings.
 #include "bra_internal.h"
+#include "sm100_ptx.cuh"
 
 namespace bra {
 namespace {
@@ -41,396 +42,495 @@ struct NormArgs {
 
 enum { SUM_W = 0, SUM_B = 1, SUM_GATE = 2, SUM_POST_W = 3, SUM_POST_B = 4, SUMS = 5 };
 
+// Eight channels of a thread as four pairs: packed fp32 arithmetic halves the instructions, which are what bounds short rows
+// (498 a round of four 64-channel rows before, at 0.63 issued per cycle and scheduler).
+struct Eight {
+    float2 v[4];
+    __device__ __forceinline__ void fill(float f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = make_float2(f, f);
+    }
+};
+__device__ __forceinline__ float2 both(float f) { return make_float2(f, f); }
+__device__ __forceinline__ float total(const Eight& a) {
+    const float2 s = __fadd2_rn(__fadd2_rn(a.v[0], a.v[1]), __fadd2_rn(a.v[2], a.v[3]));
+    return s.x + s.y;
+}
+__device__ __forceinline__ float dot(const Eight& a, const Eight& b) {
+    float2 s = __fmul2_rn(a.v[0], b.v[0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) s = __ffma2_rn(a.v[i], b.v[i], s);
+    return s.x + s.y;
+}
+
 // ---------------------------------------------------------------- a thread's eight channels of a row
 // VECD: neighbours (rows start on 16 bytes, C a multiple of eight).  Else channel j of thread t is t + j * group: neighbours over
 // the threads.
-template <typename T, bool VECD> struct Raw;
-template <> struct Raw<__nv_bfloat16, true> { uint4 v; };
-template <> struct Raw<float, true> { float4 v[2]; };
-template <typename T> struct Raw<T, false> { T v[NORM_E]; };
-
 template <bool VECD>
 struct Cols {
     int t, group, C;
+    bool any;                               // VECD: whether these channels exist, all or none
+    __device__ __forceinline__ Cols(int t_, int group_, int C_) : t(t_), group(group_), C(C_), any(t_ * NORM_E < C_) {}
     __device__ __forceinline__ int at(int j) const { return VECD ? t * NORM_E + j : t + j * group; }
-    __device__ __forceinline__ bool has(int j) const { return at(j) < C; }    // VECD: the same for every j
+    __device__ __forceinline__ bool has(int j) const { return VECD ? any : at(j) < C; }
+    // f for channels that exist, 0 for the others
+    __device__ __forceinline__ float2 only(float f, int i) const {
+        return VECD ? both(any ? f : 0.f) : make_float2(has(2 * i) ? f : 0.f, has(2 * i + 1) ? f : 0.f);
+    }
 };
 
-__device__ __forceinline__ void fetch(Raw<__nv_bfloat16, true>& r, const __nv_bfloat16* row, const Cols<true>& c) {
-    r.v = make_uint4(0, 0, 0, 0);
-    if (c.has(0)) r.v = __ldg(reinterpret_cast<const uint4*>(row + c.at(0)));
+__device__ __forceinline__ void widen(const uint32_t (&w)[4], Eight& f) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f.v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
-__device__ __forceinline__ void fetch(Raw<float, true>& r, const float* row, const Cols<true>& c) {
-    r.v[0] = r.v[1] = make_float4(0, 0, 0, 0);
-    if (c.has(0)) {
-        r.v[0] = __ldg(reinterpret_cast<const float4*>(row + c.at(0)));
-        r.v[1] = __ldg(reinterpret_cast<const float4*>(row + c.at(0)) + 1);
+
+// How far rows are read ahead: through a ring in shared memory whose 16- or 4-byte slots are each one thread's own, so that neither
+// registers nor barriers are spent on rows in flight; one slot more than rows in flight, so that none is written that was read in the
+// same round.  Rows of bf16 that start on two bytes cannot be copied so (four at least) and go through registers, one row ahead.
+// DEPTH: rows in flight, as many as shared memory has room for; 0: rows are read when it is their turn.
+template <typename T, bool VECD, int TENSORS, int DEPTH>
+struct Ahead {
+    static constexpr bool RING = DEPTH > 0 && (VECD || sizeof(T) == 4);
+    static constexpr int ROWS = RING || DEPTH == 0 ? DEPTH : 1;
+    static constexpr int CHUNKS = VECD ? NORM_E * (int)sizeof(T) / 16 : NORM_E, CHUNK = VECD ? 16 : 4;
+    static constexpr size_t bytes(int threads) { return RING ? (size_t)(DEPTH + 1) * TENSORS * NORM_E * sizeof(T) * threads : 0; }
+    T raw[RING || DEPTH == 0 ? 1 : TENSORS][NORM_E];
+    const T* row[TENSORS];                  // of the row that is fetched next, at this thread's first channel; null: no such tensor
+    uint32_t base, pitch;                   // this thread's first slot, bytes between its chunks
+    uint32_t get = 0, put = 0;              // offsets of the rows that are read and fetched next
+    __device__ __forceinline__ void restart() { get = put; }         // nothing that was fetched is left to read
+    __device__ __forceinline__ explicit Ahead(const void* smem) : base(ptx::smem_u32(smem) + threadIdx.x * CHUNK), pitch(blockDim.x * CHUNK) {}
+    __device__ __forceinline__ uint32_t step(uint32_t at) const {
+        at += TENSORS * CHUNKS * pitch;
+        return at == (DEPTH + 1) * TENSORS * CHUNKS * pitch ? 0 : at;
     }
-}
-template <typename T>
-__device__ __forceinline__ void fetch(Raw<T, false>& r, const T* row, const Cols<false>& c) {
+    // fetches a row of every tensor (live: it exists) and moves on by `stride` elements
+    __device__ __forceinline__ void fetch(bool live, long long stride, const Cols<VECD>& c) {
 #pragma unroll
-    for (int j = 0; j < NORM_E; ++j) r.v[j] = c.has(j) ? row[c.at(j)] : T(0.f);
-}
-__device__ __forceinline__ void widen(const Raw<__nv_bfloat16, true>& r, float* f) {
-    const uint32_t w[4] = {r.v.x, r.v.y, r.v.z, r.v.w};
+        for (int k = 0; k < TENSORS; ++k) {
+            if (!row[k]) continue;
+            if (live) {
+                if constexpr (RING) {
+                    const uint32_t to = base + put + k * CHUNKS * pitch;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+                    for (int j = 0; j < CHUNKS; ++j) {
+                        if constexpr (VECD) ptx::cp_async_16(to + j * pitch, c.any ? row[k] + j * (16 / (int)sizeof(T)) : row[k] - c.at(0), c.any ? 16 : 0);
+                        else ptx::cp_async_4(to + j * pitch, c.has(j) ? row[k] + j * c.group : row[k] - c.t, c.has(j) ? 4 : 0);
+                    }
+                } else if constexpr (DEPTH > 0) {
+#pragma unroll
+                    for (int j = 0; j < NORM_E; ++j) raw[k][j] = c.has(j) ? row[k][j * c.group] : T(0.f);
+                }
+            }
+            row[k] += stride;
+        }
+        if (RING) {
+            ptx::cp_async_commit();
+            put = step(put);
+        }
     }
-}
-__device__ __forceinline__ void widen(const Raw<float, true>& r, float* f) {
+    __device__ __forceinline__ void arrived() { if constexpr (RING) ptx::cp_async_wait<DEPTH - 1>(); }
+    __device__ __forceinline__ void read(int tensor, Eight& f, const Cols<VECD>& c) const {
+        if constexpr (DEPTH == 0) {
+            float v[NORM_E] = {};
+            if constexpr (VECD) {
+                if (c.any) load_row<NORM_E>(row[tensor], v);
+            } else {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        f[4 * i] = r.v[i].x; f[4 * i + 1] = r.v[i].y; f[4 * i + 2] = r.v[i].z; f[4 * i + 3] = r.v[i].w;
+                for (int j = 0; j < NORM_E; ++j) if (c.has(j)) v[j] = (float)row[tensor][j * c.group];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f.v[i] = make_float2(v[2 * i], v[2 * i + 1]);
+        } else if constexpr (RING) {
+            const uint32_t from = base + get + tensor * CHUNKS * pitch;
+            if constexpr (VECD && sizeof(T) == 2) {
+                const float4 v = ptx::lds_f32x4(from);
+                widen({__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)}, f);
+            } else if constexpr (VECD) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float4 v = ptx::lds_f32x4(from + k * pitch);
+                    f.v[2 * k] = make_float2(v.x, v.y);
+                    f.v[2 * k + 1] = make_float2(v.z, v.w);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f.v[i] = make_float2(ptx::lds_f32(from + 2 * i * pitch), ptx::lds_f32(from + (2 * i + 1) * pitch));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f.v[i] = make_float2(__bfloat162float(raw[tensor][2 * i]), __bfloat162float(raw[tensor][2 * i + 1]));
+        }
     }
-}
-__device__ __forceinline__ void widen(const Raw<float, false>& r, float* f) {
-#pragma unroll
-    for (int j = 0; j < NORM_E; ++j) f[j] = r.v[j];
-}
-__device__ __forceinline__ void widen(const Raw<__nv_bfloat16, false>& r, float* f) {
-#pragma unroll
-    for (int j = 0; j < NORM_E; ++j) f[j] = __bfloat162float(r.v[j]);
-}
+    __device__ __forceinline__ void next() { if (RING) get = step(get); }
+};
+
+// 4096 channels of fp32 backwards: 82 KB of sums and a ring of 131 KB; 8192: 164 KB of sums
+__host__ __device__ constexpr int forward_depth(int threads) { return threads <= 512 ? 3 : 2; }
+__host__ __device__ constexpr int backward_depth(int threads) { return threads <= 128 ? 3 : threads <= 512 ? 1 : 0; }
+
 template <typename T, bool VECD>
-__device__ __forceinline__ void put(T* row, const float* f, const Cols<VECD>& c) {
+__device__ __forceinline__ void put(T* row, const Eight& f, const Cols<VECD>& c) {
     if constexpr (VECD) {
-        if (c.has(0)) store_row<NORM_E>(row + c.at(0), f);
+        const float v[NORM_E] = {f.v[0].x, f.v[0].y, f.v[1].x, f.v[1].y, f.v[2].x, f.v[2].y, f.v[3].x, f.v[3].y};
+        if (c.any) store_row<NORM_E>(row + c.at(0), v);
     } else {
 #pragma unroll
-        for (int j = 0; j < NORM_E; ++j)
+        for (int j = 0; j < NORM_E; ++j) {
+            const float v = j & 1 ? f.v[j / 2].y : f.v[j / 2].x;
             if (c.has(j)) {
-                if constexpr (sizeof(T) == 2) row[c.at(j)] = __float2bfloat16_rn(f[j]);
-                else row[c.at(j)] = f[j];
+                if constexpr (sizeof(T) == 2) row[c.at(j)] = __float2bfloat16_rn(v);
+                else row[c.at(j)] = v;
             }
+        }
     }
 }
 // a vector of C floats; `none` where it is not given
 template <bool VECD>
-__device__ __forceinline__ void weights(const float* p, float none, float* f, const Cols<VECD>& c) {
-#pragma unroll
-    for (int j = 0; j < NORM_E; ++j) f[j] = none;
+__device__ __forceinline__ void weights(const float* p, float none, Eight& f, const Cols<VECD>& c) {
+    f.fill(none);
     if (!p) return;
     if constexpr (VECD) {
-        if (c.has(0)) {
+        if (c.any) {
             const float4 a = __ldg(reinterpret_cast<const float4*>(p + c.at(0))), b = __ldg(reinterpret_cast<const float4*>(p + c.at(0)) + 1);
-            f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+            f.v[0] = make_float2(a.x, a.y); f.v[1] = make_float2(a.z, a.w); f.v[2] = make_float2(b.x, b.y); f.v[3] = make_float2(b.z, b.w);
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < NORM_E; ++j) if (c.has(j)) f[j] = __ldg(p + c.at(j));
+        for (int i = 0; i < 4; ++i) {
+            if (c.has(2 * i)) f.v[i].x = __ldg(p + c.at(2 * i));
+            if (c.has(2 * i + 1)) f.v[i].y = __ldg(p + c.at(2 * i + 1));
+        }
     }
 }
 
 __device__ __forceinline__ const float* row_of(const float* p, long long off) { return p ? p + off : nullptr; }
 
 // ---------------------------------------------------------------- sums over a row
-// WIDE: the row is the CTA's.  The buffers of two consecutive sums are different ones, so that one barrier a sum is enough.
-template <bool WIDE>
+// G: lanes of a row; 0: the row is the CTA's.  The buffers of two consecutive sums are different ones, so that one barrier a sum
+// is enough.
+template <int G>
 struct RowSum {
-    int group;
-    float (*cross)[32][2];                  // [2][warps][values]
+    float2 (*cross)[32];                    // [2][warps]
     int turn = 0;
     __device__ __forceinline__ float2 of(float a, float b) {
-        const int width = WIDE ? 32 : group;
-        for (int o = width >> 1; o; o >>= 1) {
+#pragma unroll
+        for (int o = (G ? G : 32) >> 1; o; o >>= 1) {
             a += __shfl_xor_sync(0xffffffffu, a, o);
             b += __shfl_xor_sync(0xffffffffu, b, o);
         }
-        if (WIDE) {
-            const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = group >> 5;
-            if (lane == 0) { cross[turn][warp][0] = a; cross[turn][warp][1] = b; }
+        if (G == 0) {
+            const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+            if (lane == 0) cross[turn][warp] = make_float2(a, b);
             __syncthreads();
-            a = lane < warps ? cross[turn][lane][0] : 0.f;
-            b = lane < warps ? cross[turn][lane][1] : 0.f;
-            turn ^= 1;
+            if (warps <= 4) {
+                float2 s = cross[turn][0];
+                for (int w = 1; w < warps; ++w) s = __fadd2_rn(s, cross[turn][w]);
+                a = s.x; b = s.y;
+            } else {
+                const float2 s = lane < warps ? cross[turn][lane] : make_float2(0.f, 0.f);
+                a = s.x; b = s.y;
 #pragma unroll
-            for (int o = 16; o; o >>= 1) {
-                a += __shfl_xor_sync(0xffffffffu, a, o);
-                b += __shfl_xor_sync(0xffffffffu, b, o);
+                for (int o = 16; o; o >>= 1) {
+                    a += __shfl_xor_sync(0xffffffffu, a, o);
+                    b += __shfl_xor_sync(0xffffffffu, b, o);
+                }
             }
+            turn ^= 1;
         }
         return make_float2(a, b);
     }
     __device__ __forceinline__ float of(float a) {
-        const int width = WIDE ? 32 : group;
-        for (int o = width >> 1; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-        if (WIDE) {
-            const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = group >> 5;
-            if (lane == 0) cross[turn][warp][0] = a;
-            __syncthreads();
-            a = lane < warps ? cross[turn][lane][0] : 0.f;
-            turn ^= 1;
 #pragma unroll
-            for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+        for (int o = (G ? G : 32) >> 1; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+        if (G == 0) {
+            const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+            if (lane == 0) cross[turn][warp].x = a;
+            __syncthreads();
+            if (warps <= 4) {
+                a = cross[turn][0].x;
+                for (int w = 1; w < warps; ++w) a += cross[turn][w].x;
+            } else {
+                a = lane < warps ? cross[turn][lane].x : 0.f;
+#pragma unroll
+                for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+            }
+            turn ^= 1;
         }
         return a;
     }
 };
 
 // v becomes its normalised form; the factor is returned.  Channels that do not exist hold zeros and keep them.
-template <bool WIDE, bool VECD>
-__device__ __forceinline__ float normalise(int kind, float* v, const Cols<VECD>& c, float eps, RowSum<WIDE>& sum) {
+template <int G, bool VECD>
+__device__ __forceinline__ float normalise(int kind, Eight& v, const Cols<VECD>& c, float eps, float per_channel, RowSum<G>& sum) {
     if (kind == BRA_NORM_LAYER) {
-        float s = 0.f;
+        const float mean = sum.of(total(v)) * per_channel;
 #pragma unroll
-        for (int j = 0; j < NORM_E; ++j) s += v[j];
-        const float mean = sum.of(s) / (float)c.C;
-#pragma unroll
-        for (int j = 0; j < NORM_E; ++j) v[j] = c.has(j) ? v[j] - mean : 0.f;
+        for (int i = 0; i < 4; ++i) v.v[i] = __fadd2_rn(v.v[i], c.only(-mean, i));
     }
-    float s = 0.f;
+    const float r = rsqrtf(fmaf(sum.of(dot(v, v)), per_channel, eps));
 #pragma unroll
-    for (int j = 0; j < NORM_E; ++j) s = fmaf(v[j], v[j], s);
-    const float r = rsqrtf(sum.of(s) / (float)c.C + eps);
-#pragma unroll
-    for (int j = 0; j < NORM_E; ++j) v[j] *= r;
+    for (int i = 0; i < 4; ++i) v.v[i] = __fmul2_rn(v.v[i], both(r));
     return r;
 }
 
-// g becomes the gradient of the row whose normalised form hat had the gradient g
-template <bool WIDE, bool VECD>
-__device__ __forceinline__ void normalise_back(int kind, float* g, const float* hat, float r, const Cols<VECD>& c, RowSum<WIDE>& sum) {
-    float a = 0.f, b = 0.f;
+// g becomes the gradient of the row whose normalised form hat had the gradient g: r (g - hat mean(g hat) [- mean(g)])
+template <int G, bool VECD>
+__device__ __forceinline__ void normalise_back(int kind, Eight& g, const Eight& hat, float r, const Cols<VECD>& c, float per_channel, RowSum<G>& sum) {
+    float2 m = make_float2(0.f, 0.f);
+    if (kind == BRA_NORM_LAYER) m = sum.of(dot(g, hat), total(g));
+    else m.x = sum.of(dot(g, hat));
+    const float along = -r * (m.x * per_channel), mean = -r * (m.y * per_channel);
 #pragma unroll
-    for (int j = 0; j < NORM_E; ++j) { a = fmaf(g[j], hat[j], a); b += g[j]; }
-    float2 m;
-    if (kind == BRA_NORM_LAYER) m = sum.of(a, b);
-    else m = make_float2(sum.of(a), 0.f);
-    const float along = m.x / (float)c.C, mean = m.y / (float)c.C;
-#pragma unroll
-    for (int j = 0; j < NORM_E; ++j) g[j] = c.has(j) ? r * (g[j] - hat[j] * along - mean) : 0.f;
+    for (int i = 0; i < 4; ++i) g.v[i] = __ffma2_rn(g.v[i], both(r), __ffma2_rn(hat.v[i], both(along), c.only(mean, i)));
 }
 
 // ---------------------------------------------------------------- forward
-// A CTA's groups take the rows of its run in turn.  All groups make the same number of rounds (idle ones on the last row,
-// storing nothing), so that the shuffles and barriers of the sums are met by every thread.
+// A CTA's groups take the rows of its run in turn.  All groups make the same number of rounds (those without a row compute on what
+// the ring holds and store nothing), so that the shuffles and barriers of the sums are met by every thread.
 // THREADS: the most a CTA has.  Above 512 a thread has 64 registers: weights are read where they are used, row by row.
-template <typename T, bool VECD, bool WIDE, bool POST, int THREADS>
+template <typename T, bool VECD, int G, bool POST, int THREADS>
 __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormArgs a) {
     constexpr bool KEEP = THREADS <= 512;
-    __shared__ float cross[2][32][2];
-    const int groups = WIDE ? 1 : blockDim.x / a.group;
-    const int mine = WIDE ? 0 : threadIdx.x / a.group;
-    Cols<VECD> c{WIDE ? (int)threadIdx.x : (int)threadIdx.x % a.group, a.group, a.C};
-    RowSum<WIDE> sum{a.group, cross};
-    const long long first = (long long)blockIdx.x * a.run;
-    const long long last = min(first + a.run, a.rows) - 1;
-    const T *x = static_cast<const T*>(a.x), *y = static_cast<const T*>(a.y);
+    __shared__ float2 cross[2][32];
+    extern __shared__ __align__(16) char ring[];
+    const int groups = G ? THREADS / (G ? G : 1) : 1;
+    const int mine = G ? threadIdx.x / (G ? G : 1) : 0;
+    const Cols<VECD> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
+    RowSum<G> sum{cross};
+    const int first = (int)(blockIdx.x * (long long)a.run), end = (int)min((long long)first + a.run, a.rows);
+    const float per_channel = 1.f / (float)a.C;
+    const bool has_y = a.y != nullptr;
+    const long long start = (long long)(first + mine) * a.C, stride = (long long)groups * a.C;
 
-    Raw<T, VECD> rx, ry;
-    {
-        const long long row = min(first + mine, last);
-        fetch(rx, x + row * a.C, c);
-        if (y) fetch(ry, y + row * a.C, c);
-    }
+    Ahead<T, VECD, 2, forward_depth(THREADS)> in(ring);
+    in.row[0] = static_cast<const T*>(a.x) + start + c.at(0);
+    in.row[1] = has_y ? static_cast<const T*>(a.y) + start + c.at(0) : nullptr;
+    T* h = a.h ? static_cast<T*>(a.h) + start : nullptr;
+    T* n = a.n ? static_cast<T*>(a.n) + start : nullptr;
+    int ask = first + mine;
+#pragma unroll
+    for (int k = 0; k < in.ROWS; ++k, ask += groups) in.fetch(ask < end, stride, c);
     const bool per_image = a.gate_image || a.affine_image;
-    long long image_end = -1;                                 // last row whose image's weights are held
-    float gate[NORM_E], pw[NORM_E], pb[NORM_E], w[NORM_E], b[NORM_E];
+    int image_end = first + mine;                             // rows before it have the weights that are held
+    Eight gate, pw, pb, w, b;
     const float *gate_p = a.gate, *w_p = a.w, *b_p = a.b;
     if (POST && KEEP) {
         weights<VECD>(a.post_w, 1.f, pw, c);
         weights<VECD>(a.post_b, 0.f, pb, c);
     }
-    for (long long row0 = first; row0 <= last; row0 += groups) {
-        const long long row = min(row0 + mine, last);
-        const bool live = row0 + mine <= last;
-        if (row > image_end) {
-            const long long image = per_image ? row / a.N : 0;
-            gate_p = row_of(a.gate, a.gate_image ? image * a.C : 0);
-            w_p = row_of(a.w, a.affine_image ? image * a.C : 0);
-            b_p = row_of(a.b, a.affine_image ? image * a.C : 0);
+    for (int row0 = first; row0 < end; row0 += groups) {
+        const int row = row0 + mine;
+        const bool live = row < end;
+        if (row >= image_end && live) {
+            const int image = per_image ? row / a.N : 0;
+            gate_p = row_of(a.gate, a.gate_image ? (long long)image * a.C : 0);
+            w_p = row_of(a.w, a.affine_image ? (long long)image * a.C : 0);
+            b_p = row_of(a.b, a.affine_image ? (long long)image * a.C : 0);
             if (KEEP) {
                 weights<VECD>(gate_p, 1.f, gate, c);
                 weights<VECD>(w_p, 1.f, w, c);
                 weights<VECD>(b_p, 0.f, b, c);
             }
-            image_end = per_image ? (image + 1) * a.N - 1 : last;
+            image_end = per_image ? (int)min((long long)(image + 1) * a.N, (long long)end) : end;
         }
-        float v[NORM_E], u[NORM_E];
-        widen(rx, v);
-        if (y) widen(ry, u);
-        if (row0 + groups <= last) {
-            const long long next = min(row0 + groups + mine, last);
-            fetch(rx, x + next * a.C, c);
-            if (y) fetch(ry, y + next * a.C, c);
-        }
-        if (y) {
+        Eight v, u;
+        in.arrived();
+        in.read(0, v, c);
+        if (has_y) in.read(1, u, c);
+        in.fetch(ask < end, stride, c);
+        ask += groups;
+        in.next();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v.v[i] = __fmul2_rn(v.v[i], both(a.alpha));
+        if (has_y) {
             if (POST) {
-                normalise<WIDE>(a.post, u, c, a.eps, sum);
+                normalise<G>(a.post, u, c, a.eps, per_channel, sum);
                 if (!KEEP) { weights<VECD>(a.post_w, 1.f, pw, c); weights<VECD>(a.post_b, 0.f, pb, c); }
 #pragma unroll
-                for (int j = 0; j < NORM_E; ++j) u[j] = fmaf(u[j], pw[j], pb[j]);
+                for (int i = 0; i < 4; ++i) u.v[i] = __ffma2_rn(u.v[i], pw.v[i], pb.v[i]);
             }
             if (!KEEP) weights<VECD>(gate_p, 1.f, gate, c);
 #pragma unroll
-            for (int j = 0; j < NORM_E; ++j) v[j] = c.has(j) ? fmaf(gate[j], u[j], a.alpha * v[j]) : 0.f;
-        } else {
-#pragma unroll
-            for (int j = 0; j < NORM_E; ++j) v[j] *= a.alpha;
+            for (int i = 0; i < 4; ++i) v.v[i] = __ffma2_rn(gate.v[i], u.v[i], v.v[i]);
         }
-        if (a.h && live) put<T, VECD>(static_cast<T*>(a.h) + row * a.C, v, c);
-        if (a.pre != BRA_NORM_NONE) {
-            normalise<WIDE>(a.pre, v, c, a.eps, sum);
+        if (h) {
+            if (live) put<T, VECD>(h, v, c);
+            h += stride;
+        }
+        if (n) {
+            normalise<G>(a.pre, v, c, a.eps, per_channel, sum);
             if (!KEEP) { weights<VECD>(w_p, 1.f, w, c); weights<VECD>(b_p, 0.f, b, c); }
 #pragma unroll
-            for (int j = 0; j < NORM_E; ++j) v[j] = fmaf(v[j], w[j], b[j]);
-            if (live) put<T, VECD>(static_cast<T*>(a.n) + row * a.C, v, c);
+            for (int i = 0; i < 4; ++i) v.v[i] = __ffma2_rn(v.v[i], w.v[i], b.v[i]);
+            if (live) put<T, VECD>(n, v, c);
+            n += stride;
         }
     }
 }
 
 // ---------------------------------------------------------------- backward
-// KEEP: the sums over tokens stay in registers, and so do the weights.  Else (long rows, whose CTAs would have no registers left)
-// the sums are in shared memory, each word its thread's own, and the weights are read again for every row.
-template <typename T, bool VECD, bool WIDE, bool POST, int THREADS>
+// THREADS 128: the sums over tokens stay in registers, and so do the weights.  More (long rows, whose CTAs would have no registers
+// left): the sums are in shared memory, each word its thread's own, and the weights are read again for every row.
+template <typename T, bool VECD, int G, bool POST, int THREADS>
 __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a) {
-    constexpr bool KEEP = THREADS == 128, AHEAD = THREADS <= 512;
-    __shared__ float cross[2][32][2];
-    extern __shared__ float sums_sh[];      // !KEEP: [SUMS][E][threads]; KEEP and several groups: [E][threads], to join the groups
-    const int groups = WIDE ? 1 : blockDim.x / a.group;
-    const int mine = WIDE ? 0 : threadIdx.x / a.group;
-    Cols<VECD> c{WIDE ? (int)threadIdx.x : (int)threadIdx.x % a.group, a.group, a.C};
-    RowSum<WIDE> sum{a.group, cross};
-    const T *x = static_cast<const T*>(a.x), *y = static_cast<const T*>(a.y);
-    const T *dh = static_cast<const T*>(a.dh), *dn = static_cast<const T*>(a.dn);
-    const long long first = (long long)blockIdx.x * a.run;
-    const long long last = min(first + a.run, a.rows) - 1;
+    constexpr bool KEEP = THREADS == 128;
+    __shared__ float2 cross[2][32];
+    // !KEEP: [SUMS][E][threads]; KEEP and several groups: [E][threads], to join the groups; then the ring of rows
+    extern __shared__ __align__(16) float sums_sh[];
+    const int groups = G ? THREADS / (G ? G : 1) : 1;
+    const int mine = G ? threadIdx.x / (G ? G : 1) : 0;
+    const Cols<VECD> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
+    RowSum<G> sum{cross};
+    Ahead<T, VECD, 4, backward_depth(THREADS)> in(sums_sh + NORM_E * blockDim.x * (KEEP ? (G ? 1 : 0) : SUMS));
+    const bool has_y = a.y != nullptr, has_n = a.dn != nullptr;
+    const int first = (int)(blockIdx.x * (long long)a.run), last = (int)min((long long)first + a.run, a.rows) - 1;
+    const float per_channel = 1.f / (float)a.C;
 
-    float acc[KEEP ? SUMS : 1][NORM_E] = {};
-    auto shared_sum = [&](int s, int j) -> float& { return sums_sh[(s * NORM_E + j) * blockDim.x + threadIdx.x]; };
-    auto add = [&](int s, int j, float v) {
-        if constexpr (KEEP) acc[s][j] += v;
-        else shared_sum(s, j) += v;
-    };
+    Eight acc[KEEP ? SUMS : 1];
+    auto shared_sum = [&](int s, int i) -> float2& { return reinterpret_cast<float2*>(sums_sh)[(s * 4 + i) * blockDim.x + threadIdx.x]; };
     auto clear = [&](int s) {
+        if constexpr (KEEP) acc[s].fill(0.f);
+        else {
 #pragma unroll
-        for (int j = 0; j < NORM_E; ++j) {
-            if constexpr (KEEP) acc[s][j] = 0.f;
-            else shared_sum(s, j) = 0.f;
+            for (int i = 0; i < 4; ++i) shared_sum(s, i) = both(0.f);
+        }
+    };
+    // sum s += a * b
+    auto add = [&](int s, const Eight& p, const Eight& q) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (KEEP) acc[s].v[i] = __ffma2_rn(p.v[i], q.v[i], acc[s].v[i]);
+            else shared_sum(s, i) = __ffma2_rn(p.v[i], q.v[i], shared_sum(s, i));
+        }
+    };
+    auto add1 = [&](int s, const Eight& p) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (KEEP) acc[s].v[i] = __fadd2_rn(p.v[i], acc[s].v[i]);
+            else shared_sum(s, i) = __fadd2_rn(p.v[i], shared_sum(s, i));
         }
     };
     // this CTA's sum s, over its groups, into slot `slot`
     auto leave = [&](int s, long long slot) {
         float* to = a.part + ((size_t)s * a.slots + slot) * a.C;
-        if (!WIDE && KEEP) {
+        Eight t;
+        if constexpr (KEEP) t = acc[KEEP ? s : 0];
+        else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t.v[i] = shared_sum(s, i);
+        }
+        if (G && KEEP) {
+            float2* join = reinterpret_cast<float2*>(sums_sh);
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < NORM_E; ++j) sums_sh[j * blockDim.x + threadIdx.x] = acc[KEEP ? s : 0][j];
+            for (int i = 0; i < 4; ++i) join[i * THREADS + threadIdx.x] = t.v[i];
             __syncthreads();
             if (mine == 0) {
 #pragma unroll
-                for (int j = 0; j < NORM_E; ++j) {
-                    float t = 0.f;
-                    for (int g = 0; g < groups; ++g) t += sums_sh[j * blockDim.x + g * a.group + threadIdx.x];
-                    if (c.has(j)) to[c.at(j)] = t;
+                for (int i = 0; i < 4; ++i) {
+                    t.v[i] = both(0.f);
+                    for (int g = 0; g < groups; ++g) t.v[i] = __fadd2_rn(t.v[i], join[i * THREADS + g * G + threadIdx.x]);
                 }
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < NORM_E; ++j)
-                if (c.has(j)) {
-                    if constexpr (KEEP) to[c.at(j)] = acc[s][j];
-                    else to[c.at(j)] = shared_sum(s, j);
-                }
         }
+        if (mine == 0) put<float, VECD>(to, t, c);
         clear(s);
     };
     auto wants = [&](int s) { return (a.sums >> s) & 1; };
     auto of_image = [&](int s) { return s == SUM_GATE ? a.gate_image : s <= SUM_B ? a.affine_image : 0; };
-    if constexpr (!KEEP) {
 #pragma unroll
-        for (int s = 0; s < SUMS; ++s) clear(s);
-    }
+    for (int s = 0; s < SUMS; ++s) clear(s);
 
-    float gate[NORM_E], pw[NORM_E], pb[NORM_E], w[NORM_E];
+    Eight gate, pw, pb, w;
     const bool per_image = a.gate_image || a.affine_image;
-    long long begin = first;
+    int begin = first;
     while (begin <= last) {                                   // the rows of one image
-        const long long image = per_image ? begin / a.N : 0;
-        const long long end = per_image ? min((image + 1) * a.N - 1, last) : last;
-        const float* gate_p = row_of(a.gate, a.gate_image ? image * a.C : 0);
-        const float* w_p = row_of(a.w, a.affine_image ? image * a.C : 0);
+        const int image = per_image ? begin / a.N : 0;
+        const int end = per_image ? (int)min((long long)(image + 1) * a.N - 1, (long long)last) : last;
+        const float* gate_p = row_of(a.gate, a.gate_image ? (long long)image * a.C : 0);
+        const float* w_p = row_of(a.w, a.affine_image ? (long long)image * a.C : 0);
         if (KEEP) {
             weights<VECD>(gate_p, 1.f, gate, c);
             weights<VECD>(w_p, 1.f, w, c);
             if (POST) { weights<VECD>(a.post_w, 1.f, pw, c); weights<VECD>(a.post_b, 0.f, pb, c); }
         }
-        Raw<T, VECD> rx, ry, rh, rn;
-        auto get = [&](long long row) {
-            fetch(rx, x + row * a.C, c);
-            if (y) fetch(ry, y + row * a.C, c);
-            if (dh) fetch(rh, dh + row * a.C, c);
-            if (dn) fetch(rn, dn + row * a.C, c);
-        };
-        if (AHEAD) get(min(begin + mine, end));
-        for (long long row0 = begin; row0 <= end; row0 += groups) {
-            const long long row = min(row0 + mine, end);
-            const bool live = row0 + mine <= end;
-            float v[NORM_E], u[NORM_E], g[NORM_E], d[NORM_E];
-            if (!AHEAD) get(row);
-            widen(rx, v);
-            if (y) widen(ry, u);
-            if (dh) widen(rh, d);
-            else {
+        const long long start = (long long)(begin + mine) * a.C, stride = (long long)groups * a.C;
+        auto from = [&](const void* p) { return p ? static_cast<const T*>(p) + start + c.at(0) : nullptr; };
+        in.row[0] = from(a.x); in.row[1] = from(a.y); in.row[2] = from(a.dh); in.row[3] = from(a.dn);
+        T* dx = static_cast<T*>(a.dx) + start;
+        T* dy = has_y ? static_cast<T*>(a.dy) + start : nullptr;
+        int ask = begin + mine;
+        in.restart();
 #pragma unroll
-                for (int j = 0; j < NORM_E; ++j) d[j] = 0.f;
-            }
-            if (dn) widen(rn, g);
-            if (AHEAD && row0 + groups <= end) get(min(row0 + groups + mine, end));
+        for (int k = 0; k < in.ROWS; ++k, ask += groups) in.fetch(ask <= end, stride, c);
+        for (int row0 = begin; row0 <= end; row0 += groups) {
+            const bool live = row0 + mine <= end;
+            Eight v, u, g, d;
+            in.arrived();
+            in.read(0, v, c);
+            if (has_y) in.read(1, u, c);
+            if (a.dh) in.read(2, d, c);
+            else d.fill(0.f);
+            if (has_n) in.read(3, g, c);
+            in.fetch(ask <= end, stride, c);
+            ask += groups;
+            in.next();
             // !KEEP: the weights, as they are used
             auto post_weights = [&] { if (!KEEP && POST) { weights<VECD>(a.post_w, 1.f, pw, c); weights<VECD>(a.post_b, 0.f, pb, c); } };
-            float ry_factor = 0.f;
-            if (y) {
-                if (POST) ry_factor = normalise<WIDE>(a.post, u, c, a.eps, sum);
+            float u_factor = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v.v[i] = __fmul2_rn(v.v[i], both(a.alpha));
+            if (has_y) {
+                if (POST) u_factor = normalise<G>(a.post, u, c, a.eps, per_channel, sum);
                 post_weights();
                 if (!KEEP) weights<VECD>(gate_p, 1.f, gate, c);
 #pragma unroll
-                for (int j = 0; j < NORM_E; ++j)
-                    v[j] = c.has(j) ? fmaf(gate[j], POST ? fmaf(u[j], pw[j], pb[j]) : u[j], a.alpha * v[j]) : 0.f;
-            } else {
-#pragma unroll
-                for (int j = 0; j < NORM_E; ++j) v[j] *= a.alpha;
+                for (int i = 0; i < 4; ++i) v.v[i] = __ffma2_rn(gate.v[i], POST ? __ffma2_rn(u.v[i], pw.v[i], pb.v[i]) : u.v[i], v.v[i]);
             }
-            if (dn) {
-                const float r = normalise<WIDE>(a.pre, v, c, a.eps, sum);
+            if (has_n) {
+                const float r = normalise<G>(a.pre, v, c, a.eps, per_channel, sum);
                 if (!KEEP) weights<VECD>(w_p, 1.f, w, c);
-#pragma unroll
-                for (int j = 0; j < NORM_E; ++j) {
-                    if (live) {
-                        if (wants(SUM_W)) add(SUM_W, j, g[j] * v[j]);
-                        if (wants(SUM_B)) add(SUM_B, j, g[j]);
-                    }
-                    g[j] *= w[j];
+                if (live) {
+                    add(SUM_W, g, v);
+                    add1(SUM_B, g);
                 }
-                normalise_back<WIDE>(a.pre, g, v, r, c, sum);
 #pragma unroll
-                for (int j = 0; j < NORM_E; ++j) d[j] += g[j];
+                for (int i = 0; i < 4; ++i) g.v[i] = __fmul2_rn(g.v[i], w.v[i]);
+                normalise_back<G>(a.pre, g, v, r, c, per_channel, sum);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) d.v[i] = __fadd2_rn(d.v[i], g.v[i]);
             }
             // d = dH
 #pragma unroll
-            for (int j = 0; j < NORM_E; ++j) v[j] = a.alpha * d[j];
-            if (live) put<T, VECD>(static_cast<T*>(a.dx) + row * a.C, v, c);
-            if (y) {
+            for (int i = 0; i < 4; ++i) v.v[i] = __fmul2_rn(d.v[i], both(a.alpha));
+            if (live) put<T, VECD>(dx, v, c);
+            dx += stride;
+            if (has_y) {
                 post_weights();
                 if (!KEEP) weights<VECD>(gate_p, 1.f, gate, c);
+                if (live) {
+                    Eight yy = u;
+                    if (POST) {
 #pragma unroll
-                for (int j = 0; j < NORM_E; ++j) {
-                    if (live && wants(SUM_GATE)) add(SUM_GATE, j, d[j] * (POST ? fmaf(u[j], pw[j], pb[j]) : u[j]));
-                    d[j] *= gate[j];
-                    if (POST && live) {
-                        if (wants(SUM_POST_W)) add(SUM_POST_W, j, d[j] * u[j]);
-                        if (wants(SUM_POST_B)) add(SUM_POST_B, j, d[j]);
+                        for (int i = 0; i < 4; ++i) yy.v[i] = __ffma2_rn(u.v[i], pw.v[i], pb.v[i]);
                     }
+                    add(SUM_GATE, d, yy);
                 }
-                if (POST) {
 #pragma unroll
-                    for (int j = 0; j < NORM_E; ++j) d[j] = c.has(j) ? d[j] * pw[j] : 0.f;
-                    normalise_back<WIDE>(a.post, d, u, ry_factor, c, sum);
+                for (int i = 0; i < 4; ++i) d.v[i] = __fmul2_rn(d.v[i], gate.v[i]);
+                if (POST) {
+                    if (live) {
+                        add(SUM_POST_W, d, u);
+                        add1(SUM_POST_B, d);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) d.v[i] = __fmul2_rn(d.v[i], pw.v[i]);
+                    normalise_back<G>(a.post, d, u, u_factor, c, per_channel, sum);
                 }
-                if (live) put<T, VECD>(static_cast<T*>(a.dy) + row * a.C, d, c);
+                if (live) put<T, VECD>(dy, d, c);
+                dy += stride;
             }
         }
         if (per_image) {
@@ -454,29 +554,46 @@ struct JoinArgs {
     int which[SUMS];
 };
 
-// Adds the partial sums in order: 32 channels a CTA, eight threads a channel, each every eighth slot.
-__global__ void __launch_bounds__(256) norm_join_kernel(const JoinArgs a) {
-    __shared__ float part[8][33];
+// Adds the partial sums in order: 32 channels a CTA, WARPS warps that take every WARPS-th slot, eight of them in flight.
+template <int WARPS>
+__global__ void __launch_bounds__(32 * WARPS) norm_join_kernel(const JoinArgs a) {
+    __shared__ float part[WARPS][33];
     const int s = a.which[blockIdx.y];
-    const int lane = threadIdx.x & 31, eighth = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int ch = blockIdx.x * 32 + lane;
     const int images = a.image_sum[s] ? a.images : 1;
+    float* out = a.out[s];
+    pdl_wait();
     for (int image = blockIdx.z; image < images; image += gridDim.z) {
-        long long c0 = 0, c1 = a.ctas - 1, slot = 0;
+        int c0 = 0, c1 = a.ctas;                              // CTAs that left a row of sums, and the first one's slot
+        long long slot = 0;
         if (a.image_sum[s]) {
-            c0 = (long long)image * a.N / a.run;
-            c1 = ((long long)(image + 1) * a.N - 1) / a.run;
-            slot = image;
+            c0 = (int)((long long)image * a.N / a.run);
+            c1 = (int)(((long long)(image + 1) * a.N - 1) / a.run) + 1;
+            slot = image + c0;
         }
         float t = 0.f;
-        if (ch < a.C)
-            for (long long c = c0 + eighth; c <= c1; c += 8) t += a.part[((size_t)s * a.slots + slot + c) * a.C + ch];
-        part[eighth][lane] = t;
-        __syncthreads();
-        if (eighth == 0 && ch < a.C) {
+        if (ch < a.C) {
+            const float* from = a.part + ((size_t)s * a.slots + slot + warp) * a.C + ch;
+            const long long step = (long long)WARPS * a.C;
+            int left = c1 - c0 - warp;                        // every WARPS-th of them
+            for (; left > 7 * WARPS; left -= 8 * WARPS, from += 8 * step) {
+                float v[8];
 #pragma unroll
-            for (int k = 1; k < 8; ++k) t += part[k][lane];
-            a.out[s][(size_t)(a.image_sum[s] ? image : 0) * a.C + ch] = t;
+                for (int k = 0; k < 8; ++k) v[k] = __ldcg(from + k * step);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) t += v[k];
+            }
+#pragma unroll
+            for (int k = 0; k < 7; ++k)
+                if (left > k * WARPS) t += __ldcg(from + k * step);
+        }
+        part[warp][lane] = t;
+        __syncthreads();
+        if (warp == 0 && ch < a.C) {
+#pragma unroll
+            for (int k = 1; k < WARPS; ++k) t += part[k][lane];
+            out[(size_t)(a.image_sum[s] ? image : 0) * a.C + ch] = t;
         }
         __syncthreads();
     }
@@ -490,21 +607,28 @@ struct Plan {
     long long ctas;
 };
 
-Plan plan(long long rows, int C, bool backward) {
+Plan plan(const bra_norm_problem* q, bool backward) {
     Plan p;
+    const long long rows = (long long)q->B * q->N;
+    const int C = q->C;
     const int need = (C + NORM_E - 1) / NORM_E;
     p.wide = need > 32;
     if (p.wide) {
         p.group = (need + 31) / 32 * 32;
         p.threads = p.group;
     } else {
-        p.group = 1;
-        while (p.group < need) p.group <<= 1;
+        p.group = need <= 8 ? 8 : need <= 16 ? 16 : 32;
         p.threads = 128;
     }
     const int groups = p.wide ? 1 : p.threads / p.group;
-    // about as many CTAs as the GPU holds at a time (registers: 128 to 160 a thread backwards, half of that forwards)
-    long long most = (long long)kSMs * (p.threads <= 128 ? (backward ? 3 : 8) : p.threads <= 256 ? (backward ? 2 : 4) : backward ? 1 : 2);
+    // as many CTAs as an SM holds at a time, by registers and the ring
+    const bool f32 = q->dtype == BRA_F32;
+    int per_sm;
+    const bool post = q->post != BRA_NORM_NONE;
+    if (p.threads <= 128) per_sm = (backward ? (f32 || post ? 3 : 4) : (f32 || post ? 5 : 6)) * 128 / p.threads;
+    else per_sm = (backward || f32 ? 512 : 1024) / p.threads;
+    if (per_sm < 1) per_sm = 1;
+    long long most = (long long)kSMs * per_sm;
     const long long rounds = (rows + groups - 1) / groups;
     if (most > rounds) most = rounds;
     const long long each = (rounds + most - 1) / most;
@@ -541,47 +665,44 @@ long long slots_of(const bra_norm_problem* p, const Plan& pl) {
     return pl.ctas + ((p->gate == BRA_GATE_IMAGE || p->per_image) ? p->B : 0);
 }
 
-template <typename T, bool VECD, bool WIDE, int THREADS>
-cudaError_t forward_as(const NormArgs& a, const Plan& pl, cudaStream_t st) {
-    if (a.post != BRA_NORM_NONE) norm_forward_kernel<T, VECD, WIDE, true, THREADS><<<(unsigned)pl.ctas, pl.threads, 0, st>>>(a);
-    else                         norm_forward_kernel<T, VECD, WIDE, false, THREADS><<<(unsigned)pl.ctas, pl.threads, 0, st>>>(a);
-    count_launch();
-    return cudaGetLastError();
-}
-template <typename T, bool VECD>
-cudaError_t forward(const NormArgs& a, const Plan& pl, cudaStream_t st) {
-    if (!pl.wide) return forward_as<T, VECD, false, 128>(a, pl, st);
-    if (pl.threads <= 128) return forward_as<T, VECD, true, 128>(a, pl, st);
-    return pl.threads <= 512 ? forward_as<T, VECD, true, 512>(a, pl, st) : forward_as<T, VECD, true, 1024>(a, pl, st);
-}
-
-template <typename T, bool VECD, bool WIDE, bool POST, int THREADS>
-cudaError_t backward_post(const NormArgs& a, const Plan& pl, cudaStream_t st) {
-    constexpr bool KEEP = THREADS == 128;
-    const size_t smem = sizeof(float) * NORM_E * pl.threads * (KEEP ? (WIDE ? 0 : 1) : SUMS);
-    if (!KEEP) {
-        static PerDeviceMax attr;
-        const cudaError_t e = attr.ensure((int)smem, [&] {
-            return cudaFuncSetAttribute(norm_backward_kernel<T, VECD, WIDE, POST, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        });
+// Dynamic shared memory of every kernel is a constant times its threads, the most of which THREADS says: allowed once per device.
+template <typename Kernel>
+cudaError_t launch_rows(Kernel kernel, size_t smem, const NormArgs& a, const Plan& pl, cudaStream_t st) {
+    if (smem > 46 * 1024) {                 // 48 KB less what the kernels have of their own
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
-    norm_backward_kernel<T, VECD, WIDE, POST, THREADS><<<(unsigned)pl.ctas, pl.threads, smem, st>>>(a);
+    kernel<<<(unsigned)pl.ctas, pl.threads, smem, st>>>(a);
     count_launch();
     return cudaGetLastError();
 }
-template <typename T, bool VECD, bool WIDE, int THREADS>
+
+template <typename T, bool VECD, int G, int THREADS>
+cudaError_t forward_as(const NormArgs& a, const Plan& pl, cudaStream_t st) {
+    const size_t smem = Ahead<T, VECD, 2, forward_depth(THREADS)>::bytes(pl.threads);
+    return a.post != BRA_NORM_NONE ? launch_rows(norm_forward_kernel<T, VECD, G, true, THREADS>, smem, a, pl, st)
+                                   : launch_rows(norm_forward_kernel<T, VECD, G, false, THREADS>, smem, a, pl, st);
+}
+template <typename T, bool VECD, int G, int THREADS>
 cudaError_t backward_as(const NormArgs& a, const Plan& pl, cudaStream_t st) {
-    return a.post != BRA_NORM_NONE ? backward_post<T, VECD, WIDE, true, THREADS>(a, pl, st) : backward_post<T, VECD, WIDE, false, THREADS>(a, pl, st);
+    constexpr bool KEEP = THREADS == 128;
+    const size_t smem = sizeof(float) * NORM_E * pl.threads * (KEEP ? (G ? 1 : 0) : SUMS) + Ahead<T, VECD, 4, backward_depth(THREADS)>::bytes(pl.threads);
+    return a.post != BRA_NORM_NONE ? launch_rows(norm_backward_kernel<T, VECD, G, true, THREADS>, smem, a, pl, st)
+                                   : launch_rows(norm_backward_kernel<T, VECD, G, false, THREADS>, smem, a, pl, st);
 }
 template <typename T, bool VECD>
-cudaError_t backward(const NormArgs& a, const Plan& pl, cudaStream_t st) {
-    if (!pl.wide) return backward_as<T, VECD, false, 128>(a, pl, st);
-    if (pl.threads <= 128) return backward_as<T, VECD, true, 128>(a, pl, st);
-    return pl.threads <= 512 ? backward_as<T, VECD, true, 512>(a, pl, st) : backward_as<T, VECD, true, 1024>(a, pl, st);
+cudaError_t launch(bool backward, const NormArgs& a, const Plan& pl, cudaStream_t st) {
+#define BRA_NORM_AS(G, THREADS) (backward ? backward_as<T, VECD, G, THREADS>(a, pl, st) : forward_as<T, VECD, G, THREADS>(a, pl, st))
+    if (!pl.wide) return pl.group == 8 ? BRA_NORM_AS(8, 128) : pl.group == 16 ? BRA_NORM_AS(16, 128) : BRA_NORM_AS(32, 128);
+    if (pl.threads <= 128) return BRA_NORM_AS(0, 128);
+    return pl.threads <= 512 ? BRA_NORM_AS(0, 512) : BRA_NORM_AS(0, 1024);
+#undef BRA_NORM_AS
 }
-
-bool vectors(const bra_norm_problem* p) { return p->C % NORM_E == 0; }
+cudaError_t launch(bool backward, const bra_norm_problem* p, const NormArgs& a, const Plan& pl, cudaStream_t st) {
+    const bool vec = p->C % NORM_E == 0;
+    if (p->dtype == BRA_BF16) return vec ? launch<__nv_bfloat16, true>(backward, a, pl, st) : launch<__nv_bfloat16, false>(backward, a, pl, st);
+    return vec ? launch<float, true>(backward, a, pl, st) : launch<float, false>(backward, a, pl, st);
+}
 
 }  // namespace
 }  // namespace bra
@@ -592,7 +713,7 @@ extern "C" {
 
 size_t bra_norm_workspace_bytes(const bra_norm_problem* p) {
     if (check(p) != BRA_OK) return 0;
-    const Plan pl = plan((long long)p->B * p->N, p->C, true);
+    const Plan pl = plan(p, true);
     return (sizeof(float) * SUMS * (size_t)slots_of(p, pl) * p->C + 255) & ~size_t(255);
 }
 
@@ -609,14 +730,11 @@ bra_status bra_residual_norm(const bra_norm_problem* p, const void* x, const voi
     for (const void* q : {x, y, (const void*)h, (const void*)n, (const void*)gate, (const void*)post_w, (const void*)post_b, (const void*)w, (const void*)b})
         if (!aligned_to(q, 16)) return BRA_ERR_ALIGN;
     if (n == x || n == y || n == h) return BRA_ERR_UNSUPPORTED;
-    const Plan pl = plan((long long)p->B * p->N, p->C, false);
+    const Plan pl = plan(p, false);
     NormArgs a = args_of(p, pl);
     a.x = x; a.y = y; a.gate = gate; a.post_w = post_w; a.post_b = post_b; a.w = w; a.b = b; a.h = h; a.n = n;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    cudaError_t e;
-    if (p->dtype == BRA_BF16) e = vectors(p) ? forward<__nv_bfloat16, true>(a, pl, st) : forward<__nv_bfloat16, false>(a, pl, st);
-    else                      e = vectors(p) ? forward<float, true>(a, pl, st) : forward<float, false>(a, pl, st);
-    return e == cudaSuccess ? BRA_OK : BRA_ERR_CUDA;
+    return launch(false, p, a, pl, st) == cudaSuccess ? BRA_OK : BRA_ERR_CUDA;
 }
 
 bra_status bra_residual_norm_backward(const bra_norm_problem* p, const void* x, const void* y, const float* gate,
@@ -643,7 +761,7 @@ bra_status bra_residual_norm_backward(const bra_norm_problem* p, const void* x, 
     if (!ws) return BRA_ERR_NULL;
     if (!aligned_to(ws, 256)) return BRA_ERR_ALIGN;
     if (ws_bytes < bra_norm_workspace_bytes(p)) return BRA_ERR_WORKSPACE;
-    const Plan pl = plan((long long)p->B * p->N, p->C, true);
+    const Plan pl = plan(p, true);
     NormArgs a = args_of(p, pl);
     a.x = x; a.y = y; a.gate = gate; a.post_w = post_w; a.post_b = post_b; a.w = w; a.dh = dh; a.dn = dn; a.dx = dx; a.dy = dy;
     a.part = static_cast<float*>(ws);
@@ -662,15 +780,15 @@ bra_status bra_residual_norm_backward(const bra_norm_problem* p, const void* x, 
         if (of_image[k]) most_images = p->B;
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    cudaError_t e;
-    if (p->dtype == BRA_BF16) e = vectors(p) ? backward<__nv_bfloat16, true>(a, pl, st) : backward<__nv_bfloat16, false>(a, pl, st);
-    else                      e = vectors(p) ? backward<float, true>(a, pl, st) : backward<float, false>(a, pl, st);
-    if (e != cudaSuccess) return BRA_ERR_CUDA;
+    if (launch(true, p, a, pl, st) != cudaSuccess) return BRA_ERR_CUDA;
     if (wanted) {
         const dim3 grid((p->C + 31) / 32, wanted, most_images < GRID_YZ ? most_images : GRID_YZ);
-        norm_join_kernel<<<grid, 256, 0, st>>>(j);
+        // many rows of sums for each output: many warps
+        const long long each = pl.ctas / most_images;
+        const cudaError_t e = each > 64 ? launch_kernel(norm_join_kernel<32>, grid, dim3(1024), 0, st, true, j)
+                                        : launch_kernel(norm_join_kernel<8>, grid, dim3(256), 0, st, true, j);
+        if (e != cudaSuccess) return BRA_ERR_CUDA;
         count_launch();
-        if (cudaGetLastError() != cudaSuccess) return BRA_ERR_CUDA;
     }
     return BRA_OK;
 }

@@ -1,12 +1,15 @@
 // Rotary positions of projected Q and K, both in one launch.
 //
 // A pair of channels (u, v) of a token turns by the angle coordinate * freq, the same for every head of Q and K.  The angle is
-// formed in 64 bits: at coordinate 10^6 a 32-bit product is off by 0.03 turns of a radian, and B200's 64-bit rate makes it
-// cheap.  It is brought to half a turn there and only then goes to 32 bits (sincospi, no slow path).
+// formed in 64 bits (at coordinate 10^6 a 32-bit product is off by 0.03 radians), and only what is left of it without whole turns
+// goes to 32 bits.
 //
-// What bounds it: HBM, every channel read and written once.  A CTA takes a few tokens: it first puts the (cos, sin) of every pair
-// of them in shared memory - one evaluation per (token, pair), shared by all heads - and then streams the rows of all heads of Q
-// and K through 16-byte loads, four in flight per thread.
+// What bounds it: HBM, every channel read and written once.  A thread has 16 bytes of a head (half layout: and the 16 that belong to
+// them) of one token, makes the (cos, sin) of its pairs once, in registers, and walks the heads of Q and K with them - of all images,
+// where the positions are those that the problem implies - four loads in flight.  No shared memory, no barrier.  The walk is split
+// where there are too few tokens for the GPU.
+// (Measured, B200, 64 x 56 x 56 tokens, 2 + 2 heads of 32, bf16, both ways / 65537 tokens, 12 + 4 heads of 128, fp32: tables in
+// shared memory, a CTA per 64 or 2 tokens 98 / 213 us, CTAs that walk chunks of tokens 86 / 300 us.)
 #include "bra_internal.h"
 #include "fast_div.h"
 
@@ -17,20 +20,20 @@ namespace {
 
 constexpr int ROPE_THREADS = 256;
 constexpr int ROPE_AHEAD = 4;           // units in flight per thread
-constexpr int ROPE_MAX_TOKENS = 64;     // of a CTA
 
 struct RopeArgs {
     const void *Q, *K;
     void *Qo, *Ko;
     const int32_t* positions;
     const double* freq;
-    long long tokens, q_stride, k_stride;
+    long long lanes;                    // threads that are needed: tokens with a position of their own, times units
+    long long q_stride, k_stride;
     int N, heads, all_heads, D, rot, n, axes, width, first;
-    int per_cta;                        // tokens of a CTA
+    int walk, part;                     // heads (of all images, where positions are implied) of a token, and of one part of them
     float magnitude, sine;              // sine: -1 for the inverse
     bool q_in_place, k_in_place;
-    FastDiv units_div, row_div;         // units of a head, of a token's heads
-    int units, row_units;
+    int units;                          // of a head
+    FastDiv units_div, heads_div, width_div;
 };
 
 template <typename T> __device__ __forceinline__ float to_f(T v);
@@ -47,121 +50,126 @@ template <typename T, int V> struct alignas(sizeof(T) * V) Pack { T v[V]; };
 template <typename T, int VEC, bool HALF>
 struct Unit {
     static constexpr int W = HALF ? VEC : (VEC < 2 ? 2 : VEC);
+    static constexpr int PAIRS = HALF ? VEC : W / 2;
     Pack<T, VEC> a[W / VEC], b;
-    const T* src;
-    T* dst;
-    int c;                              // first channel
-    int at;                             // (cos, sin) of the first pair; -1: channels that are copied
-    bool live;
-
-    __device__ __forceinline__ void load(const RopeArgs& g, long long token0, int i, int end) {
-        live = i < end;
-        if (!live) return;
-        const int t = (int)fdiv((uint32_t)i, g.row_div), hu = i - t * g.row_units;
-        const int h = (int)fdiv((uint32_t)hu, g.units_div), u = hu - h * g.units;
-        const bool of_q = h < g.heads;
-        const long long off = (token0 + t) * (of_q ? g.q_stride : g.k_stride) + (long long)(of_q ? h : h - g.heads) * g.D;
-        src = static_cast<const T*>(of_q ? g.Q : g.K) + off;
-        dst = static_cast<T*>(of_q ? g.Qo : g.Ko) + off;
-        const bool in_place = of_q ? g.q_in_place : g.k_in_place;
+    T* dst;                             // null: nothing to do
+    // turned: pairs of the unit that turn; whole: all its channels exist
+    __device__ __forceinline__ void load(const T* src, T* to, int turned, bool whole, int half) {
+        dst = to;
         if (HALF) {
-            const int pair = u * VEC;
-            if (2 * pair < g.rot) {
-                const int half = g.n >> 1, block = pair >= half ? 1 : 0;      // at most two blocks
-                c = pair + block * half;
-                at = t * (g.rot >> 1) + pair;
-                a[0] = *reinterpret_cast<const Pack<T, VEC>*>(src + c);
-                b = *reinterpret_cast<const Pack<T, VEC>*>(src + c + half);
-            } else {
-                c = g.rot + pair - (g.rot >> 1);
-                at = -1;
-                if (in_place) { live = false; return; }
-                a[0] = *reinterpret_cast<const Pack<T, VEC>*>(src + c);
-            }
+            a[0] = *reinterpret_cast<const Pack<T, VEC>*>(src);
+            if (turned) b = *reinterpret_cast<const Pack<T, VEC>*>(src + half);
         } else {
-            c = u * W;
-            at = c < g.rot ? t * (g.rot >> 1) + (c >> 1) : -1;
-            if (at < 0 && in_place) { live = false; return; }
 #pragma unroll
             for (int k = 0; k < W / VEC; ++k)
-                if (VEC > 1 || c + k < g.D) a[k] = *reinterpret_cast<const Pack<T, VEC>*>(src + c + k * VEC);
+                if (VEC > 1 || k == 0 || whole) a[k] = *reinterpret_cast<const Pack<T, VEC>*>(src + k * VEC);
         }
     }
-    __device__ __forceinline__ void finish(const RopeArgs& g, const float2* turn) {
-        if (!live) return;
+    __device__ __forceinline__ void finish(const float2 (&cs)[PAIRS], int turned, bool whole, int half) {
         if (HALF) {
-            if (at >= 0) {
+            if (turned) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    const float2 cs = turn[at + e];
                     const float u = to_f(a[0].v[e]), v = to_f(b.v[e]);
-                    a[0].v[e] = from_f<T>(u * cs.x - v * cs.y);
-                    b.v[e] = from_f<T>(u * cs.y + v * cs.x);
+                    a[0].v[e] = from_f<T>(u * cs[e].x - v * cs[e].y);
+                    b.v[e] = from_f<T>(u * cs[e].y + v * cs[e].x);
                 }
-                *reinterpret_cast<Pack<T, VEC>*>(dst + c + (g.n >> 1)) = b;
+                *reinterpret_cast<Pack<T, VEC>*>(dst + half) = b;
             }
-            *reinterpret_cast<Pack<T, VEC>*>(dst + c) = a[0];
+            *reinterpret_cast<Pack<T, VEC>*>(dst) = a[0];
         } else {
-            if (at >= 0) {
 #pragma unroll
-                for (int e = 0; e < W; e += 2) {
-                    if (c + e >= g.rot) break;                               // the rest of a partly rotated unit
-                    const float2 cs = turn[at + e / 2];
-                    T& x = a[e / VEC].v[e % VEC];
-                    T& y = a[(e + 1) / VEC].v[(e + 1) % VEC];
+            for (int e = 0; e < PAIRS; ++e)
+                if (e < turned) {                                            // not the rest of a partly rotated unit
+                    T& x = a[2 * e / VEC].v[2 * e % VEC];
+                    T& y = a[(2 * e + 1) / VEC].v[(2 * e + 1) % VEC];
                     const float u = to_f(x), v = to_f(y);
-                    x = from_f<T>(u * cs.x - v * cs.y);
-                    y = from_f<T>(u * cs.y + v * cs.x);
+                    x = from_f<T>(u * cs[e].x - v * cs[e].y);
+                    y = from_f<T>(u * cs[e].y + v * cs[e].x);
                 }
-            }
 #pragma unroll
             for (int k = 0; k < W / VEC; ++k)
-                if (VEC > 1 || c + k < g.D) *reinterpret_cast<Pack<T, VEC>*>(dst + c + k * VEC) = a[k];
+                if (VEC > 1 || k == 0 || whole) *reinterpret_cast<Pack<T, VEC>*>(dst + k * VEC) = a[k];
         }
     }
 };
 
 template <typename T, int VEC, bool HALF>
 __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const RopeArgs g) {
-    extern __shared__ float2 turn[];                     // [tokens of the CTA][rot / 2]
-    const long long token0 = (long long)blockIdx.x * g.per_cta;
-    const int here = (int)min((long long)g.per_cta, g.tokens - token0);
-    const int pairs = g.rot >> 1, half = g.n >> 1;
+    using U = Unit<T, VEC, HALF>;
+    const long long lane = (long long)blockIdx.x * ROPE_THREADS + threadIdx.x;
+    if (lane >= g.lanes) return;
+    const long long token = g.lanes <= 0x7fffffffll ? (long long)fdiv((uint32_t)lane, g.units_div) : lane / g.units;
+    const int u = (int)(lane - token * g.units), half = g.n >> 1, pairs = g.rot >> 1;
 
-    for (int i = threadIdx.x; i < here * pairs; i += ROPE_THREADS) {
-        const int t = i / pairs, p = i - t * pairs;
-        const int axis = p >= half ? 1 : 0;
-        const long long token = token0 + t;
-        int place;
-        if (g.positions) {
-            place = __ldg(g.positions + token * g.axes + axis);
-        } else {
-            const int in_image = (int)(token % g.N);
-            place = g.axes == 1 ? g.first + in_image : axis ? in_image % g.width : in_image / g.width;
-        }
-        // turns = angle / 2 pi; the whole ones are dropped in 64 bits
-        double turns = (double)place * __ldg(g.freq + (p - axis * half)) * 0.15915494309189533577;
-        turns -= rint(turns);
-        float s, c;
-        sincospif(2.f * (float)turns, &s, &c);
-        turn[i] = make_float2(c * g.magnitude, s * g.magnitude * g.sine);
+    // the unit's first channel and pair, how many of its pairs turn
+    int c, pair, turned;
+    bool whole = true;
+    if (HALF) {
+        pair = u * VEC;
+        turned = pair < pairs ? VEC : 0;
+        c = turned ? pair + (pair >= half ? half : 0) : g.rot + pair - pairs;                 // at most two blocks
+    } else {
+        c = u * U::W;
+        pair = c >> 1;
+        turned = min(max(pairs - pair, 0), U::PAIRS);
+        whole = c + U::W <= g.D;
     }
-    __syncthreads();
+    float2 cs[U::PAIRS];
+    if (turned) {
+        const int axis = pair >= half ? 1 : 0;          // of the unit's first pair; an interleaved unit may reach into the next block
+        int place[2];
+        if (g.positions) {
+            place[0] = __ldg(g.positions + token * g.axes);
+            place[1] = g.axes == 2 ? __ldg(g.positions + token * 2 + 1) : 0;
+        } else {
+            const int row = g.axes == 2 ? (int)fdiv((uint32_t)token, g.width_div) : 0;
+            place[0] = g.axes == 2 ? row : g.first + (int)token;
+            place[1] = (int)token - row * g.width;
+        }
+#pragma unroll
+        for (int e = 0; e < U::PAIRS; ++e) {
+            if (e < turned) {
+                const int ax = HALF ? axis : (pair + e >= half ? 1 : 0);
+                // Turns per position as a fraction of 2^64: coordinate * that, modulo 2^64, is the angle without its whole turns, exactly.
+                double t = __ldg(g.freq + (pair + e - ax * half)) * 0.15915494309189533577;
+                t -= floor(t);
+                const unsigned long long step = t < 1.0 ? __double2ull_rn(t * 18446744073709551616.0) : 0ull;
+                const unsigned long long angle = (unsigned long long)(long long)(ax ? place[1] : place[0]) * step;
+                float sn, cn;
+                sincospif((float)(int)(angle >> 32) * 4.656612873077392578125e-10f, &sn, &cn);      // 2^-31 half turns, in [-1, 1)
+                cs[e] = make_float2(cn * g.magnitude, sn * g.magnitude * g.sine);
+            }
+        }
+    }
 
-    const int end = here * g.row_units;
-    for (int i = threadIdx.x; i < end; i += ROPE_THREADS * ROPE_AHEAD) {
-        Unit<T, VEC, HALF> unit[ROPE_AHEAD];
+    int j = blockIdx.y * g.part;
+    const int end = min(j + g.part, g.walk);
+    int b = (int)fdiv((uint32_t)j, g.heads_div), h = j - b * g.all_heads;
+    for (; j < end; j += ROPE_AHEAD) {
+        U unit[ROPE_AHEAD];
 #pragma unroll
-        for (int k = 0; k < ROPE_AHEAD; ++k) unit[k].load(g, token0, i + k * ROPE_THREADS, end);
+        for (int k = 0; k < ROPE_AHEAD; ++k) {
+            unit[k].dst = nullptr;
+            if (j + k < end) {
+                const bool of_q = h < g.heads;
+                if (turned || !(of_q ? g.q_in_place : g.k_in_place)) {
+                    const long long off = ((long long)b * g.N + token) * (of_q ? g.q_stride : g.k_stride) + (of_q ? h : h - g.heads) * g.D + c;
+                    unit[k].load(static_cast<const T*>(of_q ? g.Q : g.K) + off, static_cast<T*>(of_q ? g.Qo : g.Ko) + off, turned, whole, half);
+                }
+                if (++h == g.all_heads) { h = 0; ++b; }
+            }
+        }
 #pragma unroll
-        for (int k = 0; k < ROPE_AHEAD; ++k) unit[k].finish(g, turn);
+        for (int k = 0; k < ROPE_AHEAD; ++k)
+            if (unit[k].dst) unit[k].finish(cs, turned, whole, half);
     }
 }
 
 template <typename T, int VEC>
-cudaError_t launch(const RopeArgs& a, bool half, unsigned ctas, size_t smem, cudaStream_t st) {
-    if (half) rope_kernel<T, VEC, true><<<ctas, ROPE_THREADS, smem, st>>>(a);
-    else      rope_kernel<T, VEC, false><<<ctas, ROPE_THREADS, smem, st>>>(a);
+cudaError_t launch(const RopeArgs& a, bool half, dim3 ctas, cudaStream_t st) {
+    if (half) rope_kernel<T, VEC, true><<<ctas, ROPE_THREADS, 0, st>>>(a);
+    else      rope_kernel<T, VEC, false><<<ctas, ROPE_THREADS, 0, st>>>(a);
     count_launch();
     return cudaGetLastError();
 }
@@ -224,7 +232,7 @@ bra_status bra_rope(const bra_rope_problem* p, const void* Q, const void* K, con
 
     RopeArgs a;
     a.Q = Q; a.K = K; a.Qo = Qo; a.Ko = Ko; a.positions = positions; a.freq = freq;
-    a.tokens = tokens; a.q_stride = qs; a.k_stride = ks;
+    a.q_stride = qs; a.k_stride = ks;
     a.N = p->N; a.heads = p->heads; a.all_heads = p->heads + p->kv_heads; a.D = p->head_dim;
     a.rot = p->rot_dim; a.n = p->rot_dim / p->axes; a.axes = p->axes; a.width = p->width; a.first = p->first;
     a.magnitude = p->magnitude > 0.f ? p->magnitude : 1.f;
@@ -240,31 +248,37 @@ bra_status bra_rope(const bra_rope_problem* p, const void* Q, const void* K, con
     while (vec > 1 && !fits(vec)) vec >>= 1;
     const int wide = half ? vec : (vec < 2 ? 2 : vec);
     a.units = half ? a.rot / 2 / vec + (a.D - a.rot) / vec : (a.D + wide - 1) / wide;
-    a.row_units = a.units * a.all_heads;
     a.units_div = fast_div(a.units);
-    a.row_div = fast_div(a.row_units);
-    // Tokens of a CTA: four units a thread, as long as that leaves two CTAs for every SM; the table within 48 KB.
-    long long per = (ROPE_THREADS * ROPE_AHEAD + a.row_units - 1) / a.row_units;
-    per = per < tokens / (2 * kSMs) ? per : tokens / (2 * kSMs);
-    const long long room = 48 * 1024 / (8ll * (a.rot / 2));
-    if (room < 1) return BRA_ERR_UNSUPPORTED;           // more than 6144 pairs a head
-    per = per < room ? per : room;
-    per = per < ROPE_MAX_TOKENS ? per : ROPE_MAX_TOKENS;
-    a.per_cta = per < 1 ? 1 : (int)per;
-    const long long ctas = (tokens + a.per_cta - 1) / a.per_cta;
-    if (ctas > 0x7fffffffll) return BRA_ERR_SHAPE;
-    const size_t smem = sizeof(float2) * (size_t)a.per_cta * (a.rot / 2);
+    a.heads_div = fast_div(a.all_heads);
+    a.width_div = fast_div(p->width > 0 ? p->width : 1);
+    // Implied positions are the same in every image, and so are the angles.  Where tokens times units are fewer than the threads the
+    // GPU holds twice, the walk over heads and images is split, down to one round of loads a thread.
+    const long long own = positions ? tokens : p->N;
+    a.lanes = own * a.units;
+    const long long walk = positions ? a.all_heads : (long long)p->B * a.all_heads;
+    if (walk > (1 << 30)) return BRA_ERR_SHAPE;
+    a.walk = (int)walk;
+    const long long enough = 2048ll * 2 * kSMs;
+    long long parts = (enough + a.lanes - 1) / a.lanes, most = (walk + ROPE_AHEAD - 1) / ROPE_AHEAD;
+    parts = parts < most ? parts : most;
+    parts = parts < 65535 ? parts : 65535;
+    const long long rounds = (most + parts - 1) / parts;
+    a.part = (int)(rounds * ROPE_AHEAD);
+    parts = (walk + a.part - 1) / a.part;
+    const long long blocks = (a.lanes + ROPE_THREADS - 1) / ROPE_THREADS;
+    if (blocks > 0x7fffffffll) return BRA_ERR_SHAPE;
+    const dim3 ctas((unsigned)blocks, (unsigned)parts);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (p->dtype == BRA_BF16)
-        e = vec == 8 ? launch<__nv_bfloat16, 8>(a, half, (unsigned)ctas, smem, st)
-          : vec == 4 ? launch<__nv_bfloat16, 4>(a, half, (unsigned)ctas, smem, st)
-          : vec == 2 ? launch<__nv_bfloat16, 2>(a, half, (unsigned)ctas, smem, st)
-                     : launch<__nv_bfloat16, 1>(a, half, (unsigned)ctas, smem, st);
+        e = vec == 8 ? launch<__nv_bfloat16, 8>(a, half, ctas, st)
+          : vec == 4 ? launch<__nv_bfloat16, 4>(a, half, ctas, st)
+          : vec == 2 ? launch<__nv_bfloat16, 2>(a, half, ctas, st)
+                     : launch<__nv_bfloat16, 1>(a, half, ctas, st);
     else
-        e = vec == 4 ? launch<float, 4>(a, half, (unsigned)ctas, smem, st)
-          : vec == 2 ? launch<float, 2>(a, half, (unsigned)ctas, smem, st)
-                     : launch<float, 1>(a, half, (unsigned)ctas, smem, st);
+        e = vec == 4 ? launch<float, 4>(a, half, ctas, st)
+          : vec == 2 ? launch<float, 2>(a, half, ctas, st)
+                     : launch<float, 1>(a, half, ctas, st);
     return e == cudaSuccess ? BRA_OK : BRA_ERR_CUDA;
 }
 
