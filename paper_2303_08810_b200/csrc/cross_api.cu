@@ -69,6 +69,7 @@ bra_status check_ws(const CrossDims& d, const void* ws, size_t ws_bytes) {
 CrossWs cross_ws(const CrossDims& d) {
     CrossWs L;
     size_t off = 0;
+    L.status = off; off += 256;
     L.done = off;  off += align256(sizeof(int32_t) * CROSS_COUNTERS);
     L.stats = off; off += align256(sizeof(float2) * (size_t)d.B * d.kv * ((d.rows + 63) / 64 * 64));
     const size_t f = d.esize == 2 ? cross_attend_mma_part(d) : cross_attend_simt_part(d);
@@ -84,6 +85,7 @@ CrossArgs cross_args(const CrossDims& d, char* ws) {
     a.Nq = d.Nq; a.Nk = d.Nk; a.heads = d.heads; a.kv = d.kv; a.group = d.group; a.rows = d.rows;
     a.q_stride = d.q_stride; a.k_stride = d.k_stride; a.v_stride = d.v_stride; a.o_stride = d.o_stride;
     a.scale = d.scale; a.scale_log2 = d.scale * 1.4426950408889634f;
+    a.status = reinterpret_cast<int32_t*>(ws + L.status);
     a.done = reinterpret_cast<int32_t*>(ws + L.done);
     a.stats = reinterpret_cast<float2*>(ws + L.stats);
     a.part = reinterpret_cast<float*>(ws + L.part);
@@ -118,7 +120,8 @@ bra_status bra_cross_attend(const bra_cross_problem* p, const void* Q, const voi
     CrossArgs a = cross_args(d, static_cast<char*>(ws));
     a.Q = Q; a.K = K; a.V = V; a.Oo = O; a.lse = lse; a.key_len = key_len; a.key_mask = key_mask;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = d.esize == 2 ? launch_cross_attend_mma(d, a, st) : launch_cross_attend_simt(d, a, st);
+    const cudaError_t e = d.esize != 2 ? launch_cross_attend_simt(d, a, st)
+                          : cross_attend_tc_pays(d) ? launch_cross_attend_tc(d, a, st) : launch_cross_attend_mma(d, a, st);
     return e == cudaSuccess ? BRA_OK : BRA_ERR_CUDA;
 }
 

@@ -1,0 +1,415 @@
+// Cross attention of bf16 queries to an encoder's states on the 5th-generation tensor cores: many rows, many keys.
+//
+// One CTA per SM walks pairs of tiles of 128 rows of an (image, key head); its warps:
+//   warps 0-3, 4-7   softmax of the first and second tile, thread = row = lane of tensor memory
+//   warp 8           bulk tensor copies: Q of both tiles, then blocks of 128 keys and values through a ring
+//   warp 9           tcgen05.mma, one lane: S = Q K^T (128 x 128, fp32 in tensor memory), O += P V with P read from tensor memory
+// While one tile's rows turn S into P the tensor cores work for the other: PV of a block and S of the next are issued together as
+// soon as the block's P is there, so neither waits for the other's latency.  P (bf16 pairs) lies over S.  K and V of a block serve
+// both tiles; the next pair's Q is copied under the last block's softmax.
+//
+// Rows are query tokens times the heads that share a key head (the box of a bulk copy is all of a token's heads), 128 / group
+// tokens a tile; where the group does not divide 128 the last lanes of a tile are idle.
+//
+// Softmax in base 2 with a reference maximum that moves only when a row's scores outgrow it by 2^8: p may be up to 256, sums and O
+// carry the same factor, and O is rescaled in tensor memory only then (no key so far: O is zero).  P is rounded to bf16 for the
+// second product (half a step, 2^-8, per term); sums are of the unrounded p; accumulators are fp32.
+//
+// Hidden keys: their scores are replaced (not added to), their values zeroed in shared memory by the MMA warp before the product,
+// so infinities and NaN in them reach nothing.
+#include "cross_common.cuh"
+#include "tma_map.h"
+
+#include <math.h>
+
+namespace bra {
+namespace {
+
+using namespace ptx;
+
+constexpr int THREADS = 384;                    // three warpgroups: two of softmax, one whose first two warps copy and multiply
+constexpr uint32_t POLL_LIMIT = 4000000u;
+constexpr int TM_O = 256;                       // tensor memory: S / P of the tiles at 0 and 128, O at 256 and 384
+
+template <int D>
+struct Shape {
+    static constexpr int BOX = D < 64 ? D : 64;             // channels of a bulk copy: rows of 64 or 128 bytes
+    static constexpr int BOXES = D / BOX;
+    static constexpr int ROW = BOX * 2;                     // bytes
+    static constexpr int PLANE = 128 * ROW;                 // a box of 128 rows
+    static constexpr int TILE = PLANE * BOXES;
+    static constexpr int STAGES = D == 128 ? 2 : 4;         // of K and of V each
+    static constexpr uint32_t SWIZZLE = D < 64 ? 4 : 2;     // 64 or 128 bytes
+    static constexpr int OFF_K = 2 * TILE, OFF_V = OFF_K + STAGES * TILE, OFF_BAR = OFF_V + STAGES * TILE;
+    static constexpr size_t smem = OFF_BAR + 256 + 1024;    // barriers; slack for the alignment the swizzle wants
+};
+
+struct TcArgs {
+    CrossArgs a;
+    int tokens;             // of a tile: 128 / group
+    int pairs;              // tile pairs of an (image, key head)
+    int total;              // of all of them
+    FastDiv pairs_div;
+};
+
+// Which of the 128 keys from key0 on are seen, 32 a word, the same in all lanes of a warp.
+struct Seen { uint32_t w[4]; };
+__device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+// the mask's bytes of a lane (one of each word), read a block ahead of their use
+__device__ __forceinline__ uint32_t mask_bytes(const uint8_t* mask, int key0, int end, int lane) {
+    uint32_t v = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const int j = key0 + 32 * w + lane;
+        if (j < end && __ldg(mask + j)) v |= 1u << w;
+    }
+    return v;
+}
+__device__ __forceinline__ Seen seen_of(const uint8_t* mask, uint32_t bytes, int key0, int end) {
+    Seen s;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) s.w[w] = mask ? __ballot_sync(0xffffffffu, (bytes >> w) & 1) : below(end - key0 - 32 * w);
+    return s;
+}
+
+template <int D>
+__global__ void __launch_bounds__(THREADS, 1)
+cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                       const __grid_constant__ CUtensorMap map_v) {
+    using S = Shape<D>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint64_t* bar = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR);
+    uint64_t *q_full = bar, *q_empty = bar + 1, *s_ready = bar + 2, *p_ready = bar + 4, *o_done = bar + 6, *k_full = bar + 8,
+             *k_empty = k_full + S::STAGES, *v_full = k_empty + S::STAGES, *v_empty = v_full + S::STAGES;
+    uint32_t* slot = reinterpret_cast<uint32_t*>(v_empty + S::STAGES);
+    const uint32_t base = smem_u32(smem);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const CrossArgs& a = g.a;
+
+    if (threadIdx.x == 0) {
+        mbar_init(q_full, 1);
+        mbar_init(q_empty, 1);
+        for (int w = 0; w < 2; ++w) { mbar_init(s_ready + w, 1); mbar_init(p_ready + w, 128); mbar_init(o_done + w, 1); }
+        for (int s = 0; s < S::STAGES; ++s) { mbar_init(k_full + s, 1); mbar_init(k_empty + s, 1); mbar_init(v_full + s, 1); mbar_init(v_empty + s, 1); }
+        fence_mbar_init();
+    }
+    if (warp == 9) tmem_alloc(slot, 512);
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = *slot;
+    bool ok = true;
+
+    // every role walks the same tiles
+    struct Tile { int b, kvh, token0, end, blocks, both; };
+    auto tile_of = [&](int t) {
+        Tile x;
+        const int p = (int)fdiv((uint32_t)t, g.pairs_div);
+        x.token0 = (t - p * g.pairs) * 2 * g.tokens;
+        x.b = (int)fdiv((uint32_t)p, a.kv_div);
+        x.kvh = p - x.b * a.kv;
+        x.end = cross_key_end(a, x.b);
+        x.blocks = (x.end + 127) >> 7;
+        x.both = x.token0 + g.tokens < a.Nq;
+        return x;
+    };
+
+    // registers: launched with 168 a thread, 384 x 168 = 64512 = 256 x 224 + 128 x 56
+    if (warp < 8) {
+        // ------------------------------------------------ softmax
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        const int w = warp >> 2, row = threadIdx.x & 127;
+        const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const uint32_t ts = tl + w * 128, to = tl + TM_O + w * 128;
+        const float c = a.scale_log2, jump = 8.f / c;
+        const float2 c2 = make_float2(c, c);
+        const int in_token = (int)fdiv((uint32_t)row, a.group_div), head = row - in_token * a.group;
+        uint32_t n_s = 0, n_o = 0;
+        for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
+            const Tile x = tile_of(t);
+            if (w && !x.both) continue;
+            const uint8_t* mask = a.key_mask ? a.key_mask + (long long)x.b * a.Nk : nullptr;
+            const int token = x.token0 + w * g.tokens + in_token;
+            const bool live = in_token < g.tokens && token < a.Nq;
+            float m = -INFINITY, l = 0.f;
+            uint32_t bytes = mask ? mask_bytes(mask, 0, x.end, lane) : 0u;
+            for (int j = 0; j < x.blocks; ++j) {
+                const Seen seen = seen_of(mask, bytes, j * 128, x.end);
+                if (mask) bytes = mask_bytes(mask, (j + 1) * 128, x.end, lane);
+                ok = mbar_wait(s_ready + w, n_s & 1, POLL_LIMIT) && ok;
+                ++n_s;
+                tc_fence_after_sync();
+                uint32_t r[128];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) tmem_ld_32x32b_x32(ts + 32 * k, r + 32 * k);
+                tmem_ld_wait();
+                if ((seen.w[0] & seen.w[1] & seen.w[2] & seen.w[3]) != 0xffffffffu) {
+#pragma unroll
+                    for (int k = 0; k < 128; ++k)
+                        if (!((seen.w[k >> 5] >> (k & 31)) & 1)) r[k] = 0xff800000u;
+                }
+                float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < 128; k += 8) {
+                    m0 = fmax3(m0, __uint_as_float(r[k]), __uint_as_float(r[k + 1]));
+                    m1 = fmax3(m1, __uint_as_float(r[k + 2]), __uint_as_float(r[k + 3]));
+                    m2 = fmax3(m2, __uint_as_float(r[k + 4]), __uint_as_float(r[k + 5]));
+                    m3 = fmax3(m3, __uint_as_float(r[k + 6]), __uint_as_float(r[k + 7]));
+                }
+                const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+                if (j == 0) {
+                    m = top;
+                } else if (__any_sync(0xffffffffu, top - m > jump)) {
+                    // S is there, so the products before it, the last one into O among them, are done
+                    const float up = fmaxf(m, top);
+                    const float f = up == -INFINITY ? 1.f : ex2_approx((m - up) * c);
+                    m = up;
+                    l *= f;
+#pragma unroll
+                    for (int k = 0; k < D; k += 16) {
+                        uint32_t o[16];
+                        tmem_ld_32x32b_x16(to + k, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int q = 0; q < 16; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * f);
+                        tmem_st_32x32b_x16(to + k, o);
+                    }
+                }
+                const float ref = m == -INFINITY ? 0.f : m * c;
+                const float2 minus = make_float2(-ref, -ref);
+                float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+#pragma unroll
+                for (int k = 0; k < 128; k += 32) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int q = 0; q < 32; q += 4) {
+                        float2 u = __ffma2_rn(make_float2(__uint_as_float(r[k + q]), __uint_as_float(r[k + q + 1])), c2, minus);
+                        float2 v = __ffma2_rn(make_float2(__uint_as_float(r[k + q + 2]), __uint_as_float(r[k + q + 3])), c2, minus);
+                        u = make_float2(ex2_approx(u.x), ex2_approx(u.y));
+                        v = make_float2(ex2_approx(v.x), ex2_approx(v.y));
+                        s0 = __fadd2_rn(s0, u);
+                        s1 = __fadd2_rn(s1, v);
+                        p[q / 2] = pack2_bf16(u.x, u.y);
+                        p[q / 2 + 1] = pack2_bf16(v.x, v.y);
+                    }
+                    tmem_st_32x32b_x16(ts + k / 2, p);
+                }
+                l += (s0.x + s0.y) + (s1.x + s1.y);
+                tmem_st_wait();
+                tc_fence_before_sync();
+                mbar_arrive(p_ready + w);
+                if (!ok) break;
+            }
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            if (x.blocks) {
+                ok = mbar_wait(o_done + w, n_o & 1, POLL_LIMIT) && ok;
+                ++n_o;
+                tc_fence_after_sync();
+            }
+            const int h = x.kvh * a.group + head;
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.Oo) + ((long long)x.b * a.Nq + token) * a.o_stride + (long long)h * D;
+#pragma unroll
+            for (int k = 0; k < D; k += 32) {
+                uint32_t o[32];
+                if (x.blocks) {
+                    tmem_ld_32x32b_x32(to + k, o);
+                    tmem_ld_wait();
+                }
+                if (live && ok) {
+#pragma unroll
+                    for (int q = 0; q < 32; q += 8) {
+                        uint32_t v[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            v[e] = x.blocks ? pack2_bf16(__uint_as_float(o[q + 2 * e]) * inv, __uint_as_float(o[q + 2 * e + 1]) * inv) : 0u;
+                        *reinterpret_cast<uint4*>(out + k + q) = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
+                }
+            }
+            tc_fence_before_sync();
+            if (a.lse && live && ok)
+                a.lse[((long long)x.b * a.heads + h) * a.Nq + token] = l == 0.f ? -INFINITY : (m * c + log2f(l)) * 0.69314718055994531f;
+        }
+    } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == 8) {
+        // ------------------------------------------------ copies
+        if (lane == 0) {
+            uint32_t n_q = 0, n = 0;                // tiles and blocks so far
+            for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
+                const Tile x = tile_of(t);
+                if (!x.blocks) continue;
+                if (n_q) ok = mbar_wait(q_empty, (n_q - 1) & 1, POLL_LIMIT) && ok;
+                ++n_q;
+                if (!ok) break;
+                const uint32_t q_box = (uint32_t)(g.tokens * a.group * S::ROW);
+                mbar_expect_tx(q_full, q_box * S::BOXES * (1 + x.both));
+                for (int w = 0; w <= x.both; ++w)
+#pragma unroll
+                    for (int k = 0; k < S::BOXES; ++k)
+                        tma_load_4d(base + w * S::TILE + k * S::PLANE, &map_q, q_full, k * S::BOX, x.kvh * a.group, x.token0 + w * g.tokens, x.b);
+                for (int j = 0; j < x.blocks && ok; ++j, ++n) {
+                    const int s = n % S::STAGES;
+                    const uint32_t parity = (n / S::STAGES - 1) & 1;
+                    if (n >= S::STAGES) ok = mbar_wait(k_empty + s, parity, POLL_LIMIT) && ok;
+                    if (!ok) break;
+                    mbar_expect_tx(k_full + s, S::TILE);
+#pragma unroll
+                    for (int k = 0; k < S::BOXES; ++k)
+                        tma_load_4d(base + S::OFF_K + s * S::TILE + k * S::PLANE, &map_k, k_full + s, k * S::BOX, x.kvh, j * 128, x.b);
+                    if (n >= S::STAGES) ok = mbar_wait(v_empty + s, parity, POLL_LIMIT) && ok;
+                    if (!ok) break;
+                    mbar_expect_tx(v_full + s, S::TILE);
+#pragma unroll
+                    for (int k = 0; k < S::BOXES; ++k)
+                        tma_load_4d(base + S::OFF_V + s * S::TILE + k * S::PLANE, &map_v, v_full + s, k * S::BOX, x.kvh, j * 128, x.b);
+                }
+            }
+        }
+    } else if (warp == 9) {
+        // ------------------------------------------------ products
+        constexpr uint32_t IDESC_S = umma_idesc_bf16(128, 128, false, false), IDESC_O = umma_idesc_bf16(128, D, false, true);
+        uint32_t n_q = 0, n_p[2] = {0, 0};
+        uint32_t nk = 0, nv = 0;                    // blocks whose K and V have been waited for
+        auto scores = [&](int w, int stage) {
+            if (lane == 0) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t at = (uint32_t)(k * 16 / S::BOX * S::PLANE + k * 16 % S::BOX * 2);
+                    umma_ss(tmem + w * 128, umma_smem_desc(base + w * S::TILE + at, 16, 8 * S::ROW, S::SWIZZLE),
+                            umma_smem_desc(base + S::OFF_K + stage * S::TILE + at, 16, 8 * S::ROW, S::SWIZZLE), IDESC_S, k);
+                }
+                umma_commit(s_ready + w);
+            }
+        };
+        for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
+            const Tile x = tile_of(t);
+            if (!x.blocks) continue;
+            const uint8_t* mask = a.key_mask ? a.key_mask + (long long)x.b * a.Nk : nullptr;
+            uint32_t bytes = mask ? mask_bytes(mask, 0, x.end, lane) : 0u;
+            ok = mbar_wait(q_full, n_q & 1, POLL_LIMIT) && ok;
+            ++n_q;
+            ok = mbar_wait(k_full + nk % S::STAGES, (nk / S::STAGES) & 1, POLL_LIMIT) && ok;
+            if (!ok) break;
+            tc_fence_after_sync();
+            for (int w = 0; w <= x.both; ++w) scores(w, nk % S::STAGES);
+            if (lane == 0) {
+                umma_commit(k_empty + nk % S::STAGES);
+                if (x.blocks == 1) umma_commit(q_empty);
+            }
+            ++nk;
+            for (int j = 0; j < x.blocks && ok; ++j, ++nv) {
+                const int sv = nv % S::STAGES, sk = nk % S::STAGES;
+                const bool more = j + 1 < x.blocks;
+                const Seen seen = seen_of(mask, bytes, j * 128, x.end);
+                if (mask) bytes = mask_bytes(mask, (j + 1) * 128, x.end, lane);
+                ok = mbar_wait(v_full + sv, (nv / S::STAGES) & 1, POLL_LIMIT) && ok;
+                if ((seen.w[0] & seen.w[1] & seen.w[2] & seen.w[3]) != 0xffffffffu) {
+                    // values of hidden keys: zeros
+                    constexpr int CHUNKS = S::ROW / 16;
+                    for (int r = lane / CHUNKS; r < 128; r += 32 / CHUNKS)
+                        if (!((seen.w[r >> 5] >> (r & 31)) & 1)) {
+#pragma unroll
+                            for (int k = 0; k < S::BOXES; ++k)
+                                sts_f32x4(base + S::OFF_V + sv * S::TILE + k * S::PLANE + r * S::ROW + lane % CHUNKS * 16, 0.f, 0.f, 0.f, 0.f);
+                        }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                }
+                for (int w = 0; w <= x.both; ++w) {
+                    ok = mbar_wait(p_ready + w, n_p[w] & 1, POLL_LIMIT) && ok;
+                    ++n_p[w];
+                    if (!ok) break;
+                    tc_fence_after_sync();
+                    if (lane == 0) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)             // 16 keys: 8 columns of P, 16 rows of V
+                            umma_ts(tmem + TM_O + w * 128, tmem + w * 128 + k * 8,
+                                    umma_smem_desc(base + S::OFF_V + sv * S::TILE + k * 16 * S::ROW, S::BOXES > 1 ? S::PLANE : 16, 8 * S::ROW, S::SWIZZLE),
+                                    IDESC_O, j > 0 || k > 0);
+                        if (!more) umma_commit(o_done + w);
+                    }
+                    if (more) {
+                        if (w == 0) ok = mbar_wait(k_full + sk, (nk / S::STAGES) & 1, POLL_LIMIT) && ok;
+                        if (!ok) break;
+                        tc_fence_after_sync();
+                        scores(w, sk);
+                    }
+                }
+                if (lane == 0) {
+                    umma_commit(v_empty + sv);
+                    if (more) {
+                        umma_commit(k_empty + sk);
+                        if (j + 2 == x.blocks) umma_commit(q_empty);
+                    }
+                }
+                nk += more;
+            }
+        }
+    }
+    }
+    __syncwarp();
+    if (!ok) record_error(a.status, BRA_ERR_TIMEOUT, (int)blockIdx.x);
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (warp == 9) tmem_dealloc(tmem, 512);
+}
+
+// [B, tokens, heads, D] with `stride` elements from token to token; box: BOX channels x heads x tokens of one image
+bool rows_map(CUtensorMap* m, const void* base, int D, int heads, long long tokens, int B, long long stride, int box_ch, int box_heads, int box_tokens) {
+    EncodeTiledFn enc = tma_encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)tokens, (cuuint64_t)B};
+    const cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2, (cuuint64_t)(stride * tokens) * 2};
+    const cuuint32_t box[4] = {(cuuint32_t)box_ch, (cuuint32_t)box_heads, (cuuint32_t)box_tokens, 1};
+    const cuuint32_t es[4] = {1, 1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               box_ch == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+cudaError_t launch(const CrossDims& d, const CrossArgs& a, cudaStream_t st) {
+    using S = Shape<D>;
+    TcArgs g;
+    g.a = a;
+    g.tokens = 128 / d.group;
+    g.pairs = (d.Nq + 2 * g.tokens - 1) / (2 * g.tokens);
+    g.total = g.pairs * d.B * d.kv;
+    g.pairs_div = fast_div(g.pairs);
+    CUtensorMap q, k, v;
+    if (!rows_map(&q, a.Q, D, d.heads, d.Nq, d.B, d.q_stride, S::BOX, d.group, g.tokens) ||
+        !rows_map(&k, a.K, D, d.kv, d.Nk, d.B, d.k_stride, S::BOX, 1, 128) || !rows_map(&v, a.V, D, d.kv, d.Nk, d.B, d.v_stride, S::BOX, 1, 128))
+        return cudaErrorInvalidValue;
+    static PerDeviceOnce attr;
+    const cudaError_t e = attr.run([&] {
+        return cudaFuncSetAttribute(cross_attend_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::smem);
+    });
+    if (e != cudaSuccess) return e;
+    cross_attend_tc_kernel<D><<<g.total < kSMs ? g.total : kSMs, THREADS, S::smem, st>>>(g, q, k, v);
+    count_launch();
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+bool cross_attend_tc_pays(const CrossDims& d) {
+    if (d.D < 32 || d.group > 128) return false;
+    const long long pairs = (d.Nq + 2 * (128 / d.group) - 1) / (2 * (128 / d.group));
+    if (pairs * d.B * d.kv > (1 << 30)) return false;
+    static const char* force = getenv("BRA_TC");
+    if (force) return force[0] == '1';
+    return d.rows >= 128 && d.Nk >= 128;
+}
+
+cudaError_t launch_cross_attend_tc(const CrossDims& d, CrossArgs a, cudaStream_t st) {
+    switch (d.D) {
+        case 32: return launch<32>(d, a, st);
+        case 64: return launch<64>(d, a, st);
+        default: return launch<128>(d, a, st);
+    }
+}
+
+}  // namespace bra

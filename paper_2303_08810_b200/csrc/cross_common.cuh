@@ -32,6 +32,7 @@ struct CrossArgs {
     float2* stats;                                  // [B * kv][rows, padded to 64]: log2 of the softmax denominator, delta
     float* part;                                    // fp32 sums of split work
     int32_t* done;
+    int32_t* status;                                // error words (bra_device_status)
     int Nq, Nk, heads, kv, group, rows;
     long long q_stride, k_stride, v_stride, o_stride;
     float scale, scale_log2;
@@ -39,8 +40,8 @@ struct CrossArgs {
     FastDiv tiles_div, splits_div, kv_div, group_div;
 };
 
-// Scratch: counters, rows' statistics, partial sums.
-struct CrossWs { size_t done, stats, part, total; };
+// Scratch: error words, counters, rows' statistics, partial sums.
+struct CrossWs { size_t status, done, stats, part, total; };
 CrossWs cross_ws(const CrossDims& d);
 
 // How an axis that is summed over is cut where there are too few output tiles for the GPU.
@@ -55,6 +56,8 @@ inline void cross_cut(CrossArgs& a, const CrossSplit& s) {
 
 // Launchers (bf16: tensor cores; fp32: CUDA cores).  part_floats: what the scratch of their split sums holds.
 cudaError_t launch_cross_attend_mma(const CrossDims& d, CrossArgs a, cudaStream_t st);
+bool cross_attend_tc_pays(const CrossDims& d);
+cudaError_t launch_cross_attend_tc(const CrossDims& d, CrossArgs a, cudaStream_t st);
 cudaError_t launch_cross_backward_mma(const CrossDims& d, CrossArgs a, cudaStream_t st);
 cudaError_t launch_cross_attend_simt(const CrossDims& d, CrossArgs a, cudaStream_t st);
 cudaError_t launch_cross_backward_simt(const CrossDims& d, CrossArgs a, cudaStream_t st);
