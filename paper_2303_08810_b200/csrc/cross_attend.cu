@@ -241,31 +241,16 @@ __global__ void __launch_bounds__(THREADS) cross_attend_kernel(const CrossArgs a
     if (a.splits == 1) return;
 
     if (!cross_last(a.done + at.pair * a.tiles + at.tile, a.splits, &flag)) return;
-    const float* part = a.part + (at.pair * a.tiles + at.tile) * a.splits * (long long)(S::ROWS * (D + 4));
-    for (int row = warp; row < S::ROWS; row += 4) {
-        const int rr = at.tile * S::ROWS + row;
-        if (rr >= a.rows) break;
-        float top = -INFINITY;
-        for (int s = lane; s < a.splits; s += 32) top = fmaxf(top, __ldcg(part + (long long)s * (S::ROWS * (D + 4)) + row * (D + 4) + D));
-#pragma unroll
-        for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-        const float ref = top == -INFINITY ? 0.f : top * c;
-        float v[(D + 31) / 32] = {}, sum = 0.f;
-        for (int s = 0; s < a.splits; ++s) {
-            const float* from = part + (long long)s * (S::ROWS * (D + 4)) + row * (D + 4);
-            const float f = ex2_approx(__ldcg(from + D) * c - ref);
-            sum += f * __ldcg(from + D + 1);
-#pragma unroll
-            for (int k = 0; k < (D + 31) / 32; ++k)
-                if (D >= 32 || lane < D) v[k] += f * __ldcg(from + lane + 32 * k);
-        }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.Oo) + cross_row(a, at, rr, a.o_stride, D);
-#pragma unroll
-        for (int k = 0; k < (D + 31) / 32; ++k)
-            if (D >= 32 || lane < D) out[lane + 32 * k] = __float2bfloat16_rn(v[k] * inv);
-        if (a.lse && lane == 0) a.lse[cross_stat(a, at, rr)] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
-    }
+    const long long one = S::ROWS * (D + 4);
+    cross_join<D>(a.part + (at.pair * a.tiles + at.tile) * a.splits * one, one, D + 4, min(S::ROWS, a.rows - at.tile * S::ROWS), a.splits, c,
+                  reinterpret_cast<float*>(smem),
+                  [&](int row, int ch, float4 v) {
+                      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.Oo) + cross_row(a, at, at.tile * S::ROWS + row, a.o_stride, D) + 4 * ch;
+                      *reinterpret_cast<uint2*>(out) = make_uint2(pack2_bf16(v.x, v.y), pack2_bf16(v.z, v.w));
+                  },
+                  [&](int row, float ref, float sum) {
+                      if (a.lse) a.lse[cross_stat(a, at, at.tile * S::ROWS + row)] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+                  });
 }
 
 bool few_rows(const CrossDims& d) { return d.rows <= 16; }
@@ -278,7 +263,9 @@ CrossSplit split_of(const CrossDims& d) {
 template <int D, bool KEYS>
 cudaError_t launch(CrossArgs a, long long pairs, cudaStream_t st) {
     using S = Shape<D, KEYS>;
-    const size_t smem = S::smem + (a.key_mask ? ((size_t)a.split_len + 31) / 32 * 4 : 0);
+    size_t smem = S::smem + (a.key_mask ? ((size_t)a.split_len + 31) / 32 * 4 : 0);
+    const size_t join = a.splits > 1 ? sizeof(float) * S::ROWS * (a.splits + 1) : 0;
+    smem = smem > join ? smem : join;
     static PerDeviceMax attr;
     const cudaError_t e = attr.ensure((int)smem, [&] {
         return cudaFuncSetAttribute(cross_attend_kernel<D, KEYS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);

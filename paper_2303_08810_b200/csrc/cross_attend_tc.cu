@@ -3,11 +3,14 @@
 // One CTA per SM walks pairs of tiles of 128 rows of an (image, key head); its warps:
 //   warps 0-3, 4-7   softmax of the first and second tile, thread = row = lane of tensor memory
 //   warp 8           bulk tensor copies: Q of both tiles, then blocks of 128 keys and values through a ring
-//   warp 9           tcgen05.mma, one lane: S = Q K^T (128 x 128, fp32 in tensor memory), O += P V with P read from tensor memory
-// While one tile's rows turn S into P the tensor cores work for the other: PV of a block and S of the next are issued together as
-// soon as the block's P is there, so neither waits for the other's latency.  P (bf16 pairs) lies over S.  K and V of a block serve
-// both tiles; the next pair's Q is copied under the last block's softmax.
-//
+//   warps 9, 10      tcgen05.mma of the first and second tile, one lane: S = Q K^T (128 x 128, fp32 in tensor memory),
+//                    O += P V with P (bf16 pairs) read from tensor memory
+//   warp 11          zeroes the values of hidden keys in shared memory
+// What bounds it is the softmax: 128 x 128 exponentials are 1024 cycles of an SM's MUFU, the two products 750 (head dim 64) to 1040
+// (128) of its tensor pipe.  So the softmax must not wait for products.  Up to head dim 64, P has columns of its own and S of the
+// next block is made as soon as this one's is in registers; the wait for P V of the block before is over by the time P is written.
+// At 128, O of two tiles fills tensor memory, P lies over S, and S of the next block follows P V of this one; there the two warps of
+// a scheduler take turns at the exponentials, so that one has its products made meanwhile.  K and V of a block serve both tiles; the next pair's Q is copied under the last softmax.
 // Rows are query tokens times the heads that share a key head (the box of a bulk copy is all of a token's heads), 128 / group
 // tokens a tile; where the group does not divide 128 the last lanes of a tile are idle.
 //
@@ -15,8 +18,8 @@
 // carry the same factor, and O is rescaled in tensor memory only then (no key so far: O is zero).  P is rounded to bf16 for the
 // second product (half a step, 2^-8, per term); sums are of the unrounded p; accumulators are fp32.
 //
-// Hidden keys: their scores are replaced (not added to), their values zeroed in shared memory by the MMA warp before the product,
-// so infinities and NaN in them reach nothing.
+// Hidden keys: their scores are replaced (not added to), their values zeroed before the product, so infinities and NaN in them
+// reach nothing.
 #include "cross_common.cuh"
 #include "tma_map.h"
 
@@ -29,7 +32,6 @@ using namespace ptx;
 
 constexpr int THREADS = 384;                    // three warpgroups: two of softmax, one whose first two warps copy and multiply
 constexpr uint32_t POLL_LIMIT = 4000000u;
-constexpr int TM_O = 256;                       // tensor memory: S / P of the tiles at 0 and 128, O at 256 and 384
 
 template <int D>
 struct Shape {
@@ -40,8 +42,11 @@ struct Shape {
     static constexpr int TILE = PLANE * BOXES;
     static constexpr int STAGES = D == 128 ? 2 : 4;         // of K and of V each
     static constexpr uint32_t SWIZZLE = D < 64 ? 4 : 2;     // 64 or 128 bytes
+    // tensor memory: S of the tiles at 0 and 128, O from 256 on; P behind O where there is room, else over S
+    static constexpr bool APART = D <= 64;
+    static constexpr int TM_O = 256, O_STEP = APART ? 64 : 128, TM_P = APART ? 384 : 0, P_STEP = APART ? 64 : 128;
     static constexpr int OFF_K = 2 * TILE, OFF_V = OFF_K + STAGES * TILE, OFF_BAR = OFF_V + STAGES * TILE;
-    static constexpr size_t smem = OFF_BAR + 256 + 1024;    // barriers; slack for the alignment the swizzle wants
+    static constexpr size_t smem = OFF_BAR + 384 + 1024;    // barriers; slack for the alignment the swizzle wants
 };
 
 struct TcArgs {
@@ -80,18 +85,24 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint64_t* bar = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR);
-    uint64_t *q_full = bar, *q_empty = bar + 1, *s_ready = bar + 2, *p_ready = bar + 4, *o_done = bar + 6, *k_full = bar + 8,
-             *k_empty = k_full + S::STAGES, *v_full = k_empty + S::STAGES, *v_empty = v_full + S::STAGES;
-    uint32_t* slot = reinterpret_cast<uint32_t*>(v_empty + S::STAGES);
+    uint64_t *q_full = bar, *q_empty = bar + 1, *s_ready = bar + 2, *s_free = bar + 4, *p_ready = bar + 6, *pv_done = bar + 8,
+             *k_full = bar + 10, *k_empty = k_full + S::STAGES, *v_full = k_empty + S::STAGES, *v_clean = v_full + S::STAGES,
+             *v_empty = v_clean + S::STAGES, *turn = v_empty + S::STAGES;      // turn: of the four warps of each tile
+    uint32_t* slot = reinterpret_cast<uint32_t*>(turn + 8);
     const uint32_t base = smem_u32(smem);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const CrossArgs& a = g.a;
 
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
-        mbar_init(q_empty, 1);
-        for (int w = 0; w < 2; ++w) { mbar_init(s_ready + w, 1); mbar_init(p_ready + w, 128); mbar_init(o_done + w, 1); }
-        for (int s = 0; s < S::STAGES; ++s) { mbar_init(k_full + s, 1); mbar_init(k_empty + s, 1); mbar_init(v_full + s, 1); mbar_init(v_empty + s, 1); }
+        mbar_init(q_empty, 2);
+        for (int w = 0; w < 2; ++w) {
+            mbar_init(s_ready + w, 1); mbar_init(s_free + w, 128); mbar_init(p_ready + w, 128); mbar_init(pv_done + w, 1);
+        }
+        for (int s = 0; s < S::STAGES; ++s) {
+            mbar_init(k_full + s, 1); mbar_init(k_empty + s, 2); mbar_init(v_full + s, 1); mbar_init(v_clean + s, 1); mbar_init(v_empty + s, 2);
+        }
+        for (int i = 0; i < 8; ++i) mbar_init(turn + i, 1);
         fence_mbar_init();
     }
     if (warp == 9) tmem_alloc(slot, 512);
@@ -121,11 +132,11 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int w = warp >> 2, row = threadIdx.x & 127;
         const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t ts = tl + w * 128, to = tl + TM_O + w * 128;
+        const uint32_t ts = tl + w * 128, to = tl + S::TM_O + w * S::O_STEP, tp = tl + S::TM_P + w * S::P_STEP;
         const float c = a.scale_log2, jump = 8.f / c;
         const float2 c2 = make_float2(c, c);
         const int in_token = (int)fdiv((uint32_t)row, a.group_div), head = row - in_token * a.group;
-        uint32_t n_s = 0, n_o = 0;
+        uint32_t n_s = 0, n_turn = 0;           // blocks so far; those of pairs with two tiles
         for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
             const Tile x = tile_of(t);
             if (w && !x.both) continue;
@@ -135,16 +146,23 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
             float m = -INFINITY, l = 0.f;
             uint32_t bytes = mask ? mask_bytes(mask, 0, x.end, lane) : 0u;
             for (int j = 0; j < x.blocks; ++j) {
-                const Seen seen = seen_of(mask, bytes, j * 128, x.end);
-                if (mask) bytes = mask_bytes(mask, (j + 1) * 128, x.end, lane);
-                ok = mbar_wait(s_ready + w, n_s & 1, POLL_LIMIT) && ok;
-                ++n_s;
+                const bool cut = mask || (j + 1) * 128 > x.end;       // some keys may be hidden
+                Seen seen;
+                if (cut) {
+                    seen = seen_of(mask, bytes, j * 128, x.end);
+                    if (mask) bytes = mask_bytes(mask, (j + 1) * 128, x.end, lane);
+                }
+                if (!mbar_try_wait(s_ready + w, n_s & 1)) ok = mbar_wait(s_ready + w, n_s & 1, POLL_LIMIT) && ok;
                 tc_fence_after_sync();
                 uint32_t r[128];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) tmem_ld_32x32b_x32(ts + 32 * k, r + 32 * k);
                 tmem_ld_wait();
-                if ((seen.w[0] & seen.w[1] & seen.w[2] & seen.w[3]) != 0xffffffffu) {
+                if (S::APART) {
+                    tc_fence_before_sync();
+                    mbar_arrive(s_free + w);
+                }
+                if (cut) {
 #pragma unroll
                     for (int k = 0; k < 128; ++k)
                         if (!((seen.w[k >> 5] >> (k & 31)) & 1)) r[k] = 0xff800000u;
@@ -158,10 +176,19 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
                     m3 = fmax3(m3, __uint_as_float(r[k + 6]), __uint_as_float(r[k + 7]));
                 }
                 const float top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+                // P V of the block before is done: O may be read and (where P is apart) P written.  With P over S, S says so.
+                bool waited = !S::APART || j == 0;
+                auto wait_pv = [&] {
+                    if (!waited) {
+                        if (!mbar_try_wait(pv_done + w, (n_s - 1) & 1)) ok = mbar_wait(pv_done + w, (n_s - 1) & 1, POLL_LIMIT) && ok;
+                        tc_fence_after_sync();
+                        waited = true;
+                    }
+                };
                 if (j == 0) {
                     m = top;
                 } else if (__any_sync(0xffffffffu, top - m > jump)) {
-                    // S is there, so the products before it, the last one into O among them, are done
+                    wait_pv();
                     const float up = fmaxf(m, top);
                     const float f = up == -INFINITY ? 1.f : ex2_approx((m - up) * c);
                     m = up;
@@ -175,6 +202,13 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
                         for (int q = 0; q < 16; ++q) o[q] = __float_as_uint(__uint_as_float(o[q]) * f);
                         tmem_st_32x32b_x16(to + k, o);
                     }
+                }
+                // Turns at the exponentials: 2 x 4133 x 4096, 37 heads of 128, 755 -> 690 us.  (With P apart, where nothing else waits
+                // for products, the hand-over costs more than it gives: 468 -> 519 us at 64.)
+                if (!S::APART && x.both) {
+                    if ((w || n_turn) && !mbar_try_wait(turn + warp, (w ? n_turn : n_turn - 1) & 1))
+                        ok = mbar_wait(turn + warp, (w ? n_turn : n_turn - 1) & 1, POLL_LIMIT) && ok;
+                    ++n_turn;
                 }
                 const float ref = m == -INFINITY ? 0.f : m * c;
                 const float2 minus = make_float2(-ref, -ref);
@@ -193,18 +227,23 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
                         p[q / 2] = pack2_bf16(u.x, u.y);
                         p[q / 2 + 1] = pack2_bf16(v.x, v.y);
                     }
-                    tmem_st_32x32b_x16(ts + k / 2, p);
+                    if (k == 0) wait_pv();
+                    tmem_st_32x32b_x16(tp + k / 2, p);
+                }
+                if (!S::APART && x.both) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(turn + (warp ^ 4));
                 }
                 l += (s0.x + s0.y) + (s1.x + s1.y);
                 tmem_st_wait();
                 tc_fence_before_sync();
                 mbar_arrive(p_ready + w);
+                ++n_s;
                 if (!ok) break;
             }
             const float inv = l == 0.f ? 0.f : 1.f / l;
             if (x.blocks) {
-                ok = mbar_wait(o_done + w, n_o & 1, POLL_LIMIT) && ok;
-                ++n_o;
+                ok = mbar_wait(pv_done + w, (n_s - 1) & 1, POLL_LIMIT) && ok;
                 tc_fence_after_sync();
             }
             const int h = x.kvh * a.group + head;
@@ -267,13 +306,20 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
                 }
             }
         }
-    } else if (warp == 9) {
+    } else if (warp < 11) {
         // ------------------------------------------------ products
         constexpr uint32_t IDESC_S = umma_idesc_bf16(128, 128, false, false), IDESC_O = umma_idesc_bf16(128, D, false, true);
-        uint32_t n_q = 0, n_p[2] = {0, 0};
-        uint32_t nk = 0, nv = 0;                    // blocks whose K and V have been waited for
-        auto scores = [&](int w, int stage) {
-            if (lane == 0) {
+        const int w = warp - 9;
+        uint32_t n_q = 0, nb = 0, nk = 0, nv = 0;   // tiles with keys, this tile's blocks so far; ring positions of K and V
+        // The second tile's warp follows the ring through pairs that have only one, without products: a wait two phases ahead of a
+        // barrier would not be one.
+        bool idle = false;
+        auto scores = [&] {
+            const int stage = nk % S::STAGES;
+            ok = mbar_wait(k_full + stage, (nk / S::STAGES) & 1, POLL_LIMIT) && ok;
+            if (!ok) return;
+            tc_fence_after_sync();
+            if (lane == 0 && !idle) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     const uint32_t at = (uint32_t)(k * 16 / S::BOX * S::PLANE + k * 16 % S::BOX * 2);
@@ -282,31 +328,69 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
                 }
                 umma_commit(s_ready + w);
             }
+            ++nk;
+        };
+        // stages are given back by both warps
+        auto after_scores = [&](const Tile& x, int j) {
+            if (lane == 0) {
+                umma_commit(k_empty + (nk - 1) % S::STAGES);
+                if (j + 1 == x.blocks) umma_commit(q_empty);
+            }
         };
         for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
             const Tile x = tile_of(t);
             if (!x.blocks) continue;
-            const uint8_t* mask = a.key_mask ? a.key_mask + (long long)x.b * a.Nk : nullptr;
-            uint32_t bytes = mask ? mask_bytes(mask, 0, x.end, lane) : 0u;
+            idle = w && !x.both;
             ok = mbar_wait(q_full, n_q & 1, POLL_LIMIT) && ok;
             ++n_q;
-            ok = mbar_wait(k_full + nk % S::STAGES, (nk / S::STAGES) & 1, POLL_LIMIT) && ok;
             if (!ok) break;
-            tc_fence_after_sync();
-            for (int w = 0; w <= x.both; ++w) scores(w, nk % S::STAGES);
-            if (lane == 0) {
-                umma_commit(k_empty + nk % S::STAGES);
-                if (x.blocks == 1) umma_commit(q_empty);
-            }
-            ++nk;
-            for (int j = 0; j < x.blocks && ok; ++j, ++nv) {
-                const int sv = nv % S::STAGES, sk = nk % S::STAGES;
+            scores();
+            if (!ok) break;
+            after_scores(x, 0);
+            for (int j = 0; j < x.blocks && ok; ++j, ++nv, nb += !idle) {
+                const int sv = nv % S::STAGES;
                 const bool more = j + 1 < x.blocks;
-                const Seen seen = seen_of(mask, bytes, j * 128, x.end);
-                if (mask) bytes = mask_bytes(mask, (j + 1) * 128, x.end, lane);
+                if (S::APART && more) {                         // S of this block is in registers
+                    if (!idle) ok = mbar_wait(s_free + w, nb & 1, POLL_LIMIT) && ok;
+                    if (ok) scores();
+                    if (!ok) break;
+                    after_scores(x, j + 1);
+                }
+                ok = mbar_wait(v_clean + sv, (nv / S::STAGES) & 1, POLL_LIMIT) && ok;
+                if (!idle) ok = mbar_wait(p_ready + w, nb & 1, POLL_LIMIT) && ok;
+                if (!ok) break;
+                tc_fence_after_sync();
+                if (lane == 0 && !idle) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)                 // 16 keys: 8 columns of P, 16 rows of V
+                        umma_ts(tmem + S::TM_O + w * S::O_STEP, tmem + S::TM_P + w * S::P_STEP + k * 8,
+                                umma_smem_desc(base + S::OFF_V + sv * S::TILE + k * 16 * S::ROW, S::BOXES > 1 ? S::PLANE : 16, 8 * S::ROW, S::SWIZZLE),
+                                IDESC_O, j > 0 || k > 0);
+                }
+                if (lane == 0) {
+                    if (!idle) umma_commit(pv_done + w);
+                    umma_commit(v_empty + sv);
+                }
+                if (!S::APART && more) {
+                    scores();
+                    if (!ok) break;
+                    after_scores(x, j + 1);
+                }
+            }
+            // with no next block nobody waits for it, but the phase counts
+            if (S::APART && ok && !idle) ok = mbar_wait(s_free + w, (nb - 1) & 1, POLL_LIMIT) && ok;
+        }
+    } else {
+        // ------------------------------------------------ values of hidden keys
+        uint32_t nv = 0;
+        for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
+            const Tile x = tile_of(t);
+            const uint8_t* mask = a.key_mask ? a.key_mask + (long long)x.b * a.Nk : nullptr;
+            for (int j = 0; j < x.blocks && ok; ++j, ++nv) {
+                const int sv = nv % S::STAGES;
+                const Seen seen = seen_of(mask, mask ? mask_bytes(mask, j * 128, x.end, lane) : 0u, j * 128, x.end);
                 ok = mbar_wait(v_full + sv, (nv / S::STAGES) & 1, POLL_LIMIT) && ok;
                 if ((seen.w[0] & seen.w[1] & seen.w[2] & seen.w[3]) != 0xffffffffu) {
-                    // values of hidden keys: zeros
                     constexpr int CHUNKS = S::ROW / 16;
                     for (int r = lane / CHUNKS; r < 128; r += 32 / CHUNKS)
                         if (!((seen.w[r >> 5] >> (r & 31)) & 1)) {
@@ -315,36 +399,9 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
                                 sts_f32x4(base + S::OFF_V + sv * S::TILE + k * S::PLANE + r * S::ROW + lane % CHUNKS * 16, 0.f, 0.f, 0.f, 0.f);
                         }
                     fence_proxy_async_smem();
-                    __syncwarp();
                 }
-                for (int w = 0; w <= x.both; ++w) {
-                    ok = mbar_wait(p_ready + w, n_p[w] & 1, POLL_LIMIT) && ok;
-                    ++n_p[w];
-                    if (!ok) break;
-                    tc_fence_after_sync();
-                    if (lane == 0) {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)             // 16 keys: 8 columns of P, 16 rows of V
-                            umma_ts(tmem + TM_O + w * 128, tmem + w * 128 + k * 8,
-                                    umma_smem_desc(base + S::OFF_V + sv * S::TILE + k * 16 * S::ROW, S::BOXES > 1 ? S::PLANE : 16, 8 * S::ROW, S::SWIZZLE),
-                                    IDESC_O, j > 0 || k > 0);
-                        if (!more) umma_commit(o_done + w);
-                    }
-                    if (more) {
-                        if (w == 0) ok = mbar_wait(k_full + sk, (nk / S::STAGES) & 1, POLL_LIMIT) && ok;
-                        if (!ok) break;
-                        tc_fence_after_sync();
-                        scores(w, sk);
-                    }
-                }
-                if (lane == 0) {
-                    umma_commit(v_empty + sv);
-                    if (more) {
-                        umma_commit(k_empty + sk);
-                        if (j + 2 == x.blocks) umma_commit(q_empty);
-                    }
-                }
-                nk += more;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(v_clean + sv);
             }
         }
     }
@@ -395,13 +452,19 @@ cudaError_t launch(const CrossDims& d, const CrossArgs& a, cudaStream_t st) {
 
 }  // namespace
 
+// Measured (B200, us, this kernel / the warp-level one).  One block of keys: 8 pairs of tiles of 8 heads of 32 6.4 / 3.4, 64 pairs
+// 6.1 / 4.8, 128 pairs 6.2 / 6.6, 512 pairs 16.7 / 18.2 (64 x 196 x 100).  Two blocks: 8 to 128 pairs 7.7 - 8.0 / 6.5 - 9.6; more:
+// 16 x 1024 x 1024, 12 heads of 64 97 / 195, 2 x 4133 x 4096, 37 heads of 32 474 / 744, of 64 480 / 1138, of 128 643 / 2056.
+// Few pairs and many blocks, where the other one splits the keys: 1 x 196 x 1024, 8 heads of 32 17.4 / 10.5, 2 images 17.5 / 16.0,
+// 4 images 17.5 / 15.9, 16 images 18.1 / 27.1; 1 x 100 x 2048, 8 heads of 64 22.8 / 19.0; at head dim 128 it pays all the same (1 x 1024 x
+// 2048, 4 heads 39.6 / 56.2).
 bool cross_attend_tc_pays(const CrossDims& d) {
-    if (d.D < 32 || d.group > 128) return false;
-    const long long pairs = (d.Nq + 2 * (128 / d.group) - 1) / (2 * (128 / d.group));
-    if (pairs * d.B * d.kv > (1 << 30)) return false;
-    static const char* force = getenv("BRA_TC");
-    if (force) return force[0] == '1';
-    return d.rows >= 128 && d.Nk >= 128;
+    if (d.D < 32 || d.group > 128 || d.rows <= 64) return false;
+    const int tokens = 128 / d.group;
+    const long long pairs = ((long long)d.Nq + 2 * tokens - 1) / (2 * tokens) * d.B * d.kv;
+    if (pairs > (1 << 30)) return false;
+    if (d.Nk <= 128) return pairs >= 128;
+    return d.Nk <= 896 || pairs > 16 || d.D == 128;
 }
 
 cudaError_t launch_cross_attend_tc(const CrossDims& d, CrossArgs a, cudaStream_t st) {

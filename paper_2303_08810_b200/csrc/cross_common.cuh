@@ -143,6 +143,45 @@ __device__ __forceinline__ bool cross_last(int32_t* counter, int parts, int* fla
     return *flag != 0;
 }
 
+// The parts of split rows: `rows` rows of D sums, then the reference maximum (raw score) and the sum of a row, `pitch` floats apart, a
+// part `part` floats behind the one before.  Adds them in order and writes the rows.  weight: shared memory, rows x splits floats and
+// rows more.  done(row, value index / 4, values) stores four channels, lse(row, log2 of the sum, whether there is one).
+template <int D, typename Done, typename Lse>
+__device__ __forceinline__ void cross_join(const float* parts, long long part, int pitch, int rows, int splits, float c, float* weight, Done&& done, Lse&& lse) {
+    float* inv = weight + rows * splits;
+    for (int r = threadIdx.x; r < rows; r += blockDim.x) {
+        const float* row = parts + r * pitch + D;
+        float top = -INFINITY, sum = 0.f;
+        for (int s = 0; s < splits; ++s) {
+            const float2 v = __ldcg(reinterpret_cast<const float2*>(row + s * part));
+            weight[r * splits + s] = v.x;
+            top = fmaxf(top, v.x);
+        }
+        const float ref = top == -INFINITY ? 0.f : top * c;
+        for (int s = 0; s < splits; ++s) {
+            const float f = exp2f(fmaf(weight[r * splits + s], c, -ref));
+            weight[r * splits + s] = f;
+            sum = fmaf(f, __ldcg(row + s * part + 1), sum);
+        }
+        inv[r] = sum == 0.f ? 0.f : 1.f / sum;
+        lse(r, ref, sum);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * (D / 4); i += blockDim.x) {
+        const int r = i / (D / 4), ch = i % (D / 4);
+        const float* at = parts + r * pitch + 4 * ch;
+        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+        for (int s = 0; s < splits; ++s) {
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(at + s * part));
+            const float f = weight[r * splits + s];
+            t.x = fmaf(f, v.x, t.x); t.y = fmaf(f, v.y, t.y); t.z = fmaf(f, v.z, t.z); t.w = fmaf(f, v.w, t.w);
+        }
+        const float k = inv[r];
+        done(r, ch, make_float4(t.x * k, t.y * k, t.z * k, t.w * k));
+    }
+}
+
 // ---------------------------------------------------------------- rows of D bf16 channels in shared memory
 // Chunks of 16 bytes, exclusive-or'ed with the row so that the eight rows of an ldmatrix matrix lie in different banks.
 template <int D>

@@ -190,29 +190,14 @@ __global__ void __launch_bounds__(THREADS) cross_attend_simt_kernel(const CrossA
         }
     }
     if (a.splits == 1 || !cross_last(a.done + at.pair * a.tiles + at.tile, a.splits, &flag)) return;
-    const float* part = a.part + (at.pair * a.tiles + at.tile) * a.splits * (long long)(BM * S::LD);
-    for (int row = threadIdx.x >> 5; row < BM; row += THREADS / 32) {
-        const int r = at.tile * BM + row, lane = threadIdx.x & 31;
-        if (r >= a.rows) break;
-        float top = -INFINITY;
-        for (int sp = 0; sp < a.splits; ++sp) top = fmaxf(top, __ldcg(part + sp * (long long)(BM * S::LD) + row * S::LD + D));
-        const float ref = top == -INFINITY ? 0.f : top * c;
-        float v[(D + 31) / 32] = {}, sum = 0.f;
-        for (int sp = 0; sp < a.splits; ++sp) {
-            const float* from = part + sp * (long long)(BM * S::LD) + row * S::LD;
-            const float f = exp2f(fmaf(__ldcg(from + D), c, -ref));
-            sum += f * __ldcg(from + D + 1);
-#pragma unroll
-            for (int k = 0; k < (D + 31) / 32; ++k)
-                if (D >= 32 || lane < D) v[k] += f * __ldcg(from + lane + 32 * k);
-        }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        float* out = static_cast<float*>(a.Oo) + cross_row(a, at, r, a.o_stride, D);
-#pragma unroll
-        for (int k = 0; k < (D + 31) / 32; ++k)
-            if (D >= 32 || lane < D) out[lane + 32 * k] = v[k] * inv;
-        if (a.lse && lane == 0) a.lse[cross_stat(a, at, r)] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
-    }
+    const long long one = BM * S::LD;
+    cross_join<D>(a.part + (at.pair * a.tiles + at.tile) * a.splits * one, one, S::LD, min(BM, a.rows - at.tile * BM), a.splits, c, sh,
+                  [&](int row, int ch, float4 v) {
+                      *reinterpret_cast<float4*>(static_cast<float*>(a.Oo) + cross_row(a, at, at.tile * BM + row, a.o_stride, D) + 4 * ch) = v;
+                  },
+                  [&](int row, float ref, float sum) {
+                      if (a.lse) a.lse[cross_stat(a, at, at.tile * BM + row)] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+                  });
 }
 
 // ---------------------------------------------------------------- gradients
@@ -378,7 +363,9 @@ cudaError_t forward(const CrossDims& d, CrossArgs a, cudaStream_t st) {
     using S = Shape<D, D == 128 ? 32 : 64, RI>;
     static PerDeviceMax attr;
     cross_cut(a, forward_split(d));
-    const size_t smem = sizeof(float) * (S::BM * S::LD + 2 * S::BN * S::LD + S::BM * S::LP) + mask_bytes(a, a.split_len);
+    size_t smem = sizeof(float) * (S::BM * S::LD + 2 * S::BN * S::LD + S::BM * S::LP) + mask_bytes(a, a.split_len);
+    const size_t join = a.splits > 1 ? sizeof(float) * S::BM * (a.splits + 1) : 0;
+    smem = smem > join ? smem : join;
     return launch(cross_attend_simt_kernel<D, RI>, attr, a, (long long)d.B * d.kv, smem, st);
 }
 template <int D, bool DKV>
