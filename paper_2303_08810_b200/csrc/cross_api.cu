@@ -71,7 +71,8 @@ CrossWs cross_ws(const CrossDims& d) {
     size_t off = 0;
     L.status = off; off += 256;
     L.done = off;  off += align256(sizeof(int32_t) * CROSS_COUNTERS);
-    L.stats = off; off += align256(sizeof(float2) * (size_t)d.B * d.kv * ((d.rows + 63) / 64 * 64));
+    const size_t padded = sizeof(float2) * (size_t)d.B * d.kv * ((d.rows + 63) / 64 * 64), tc = cross_backward_tc_pays(d) ? cross_backward_tc_stats(d) : 0;
+    L.stats = off; off += align256(padded > tc ? padded : tc);
     const size_t f = d.esize == 2 ? cross_attend_mma_part(d) : cross_attend_simt_part(d);
     const size_t b = d.esize == 2 ? cross_backward_mma_part(d) : cross_backward_simt_part(d);
     L.part = off;  off += align256(sizeof(float) * (f > b ? f : b));
@@ -143,7 +144,8 @@ bra_status bra_cross_backward(const bra_cross_problem* p, const void* Q, const v
     a.Q = Q; a.K = K; a.V = V; a.O = O; a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV;
     a.lse = const_cast<float*>(lse); a.key_len = key_len; a.key_mask = key_mask;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = d.esize == 2 ? launch_cross_backward_mma(d, a, st) : launch_cross_backward_simt(d, a, st);
+    const cudaError_t e = d.esize != 2 ? launch_cross_backward_simt(d, a, st)
+                          : cross_backward_tc_pays(d) ? launch_cross_backward_tc(d, a, st) : launch_cross_backward_mma(d, a, st);
     return e == cudaSuccess ? BRA_OK : BRA_ERR_CUDA;
 }
 

@@ -20,18 +20,16 @@
 //
 // Hidden keys: their scores are replaced (not added to), their values zeroed before the product, so infinities and NaN in them
 // reach nothing.
-#include "cross_common.cuh"
-#include "tma_map.h"
+#include "cross_tc_common.cuh"
 
 #include <math.h>
 
 namespace bra {
 namespace {
 
-using namespace ptx;
+using namespace cross_tc;
 
 constexpr int THREADS = 384;                    // three warpgroups: two of softmax, one whose first two warps copy and multiply
-constexpr uint32_t POLL_LIMIT = 4000000u;
 
 template <int D>
 struct Shape {
@@ -56,26 +54,6 @@ struct TcArgs {
     int total;              // of all of them
     FastDiv pairs_div;
 };
-
-// Which of the 128 keys from key0 on are seen, 32 a word, the same in all lanes of a warp.
-struct Seen { uint32_t w[4]; };
-__device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
-// the mask's bytes of a lane (one of each word), read a block ahead of their use
-__device__ __forceinline__ uint32_t mask_bytes(const uint8_t* mask, int key0, int end, int lane) {
-    uint32_t v = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const int j = key0 + 32 * w + lane;
-        if (j < end && __ldg(mask + j)) v |= 1u << w;
-    }
-    return v;
-}
-__device__ __forceinline__ Seen seen_of(const uint8_t* mask, uint32_t bytes, int key0, int end) {
-    Seen s;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) s.w[w] = mask ? __ballot_sync(0xffffffffu, (bytes >> w) & 1) : below(end - key0 - 32 * w);
-    return s;
-}
 
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1)
@@ -152,7 +130,7 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
                     seen = seen_of(mask, bytes, j * 128, x.end);
                     if (mask) bytes = mask_bytes(mask, (j + 1) * 128, x.end, lane);
                 }
-                if (!mbar_try_wait(s_ready + w, n_s & 1)) ok = mbar_wait(s_ready + w, n_s & 1, POLL_LIMIT) && ok;
+                wait_for(s_ready + w, n_s & 1, ok);
                 tc_fence_after_sync();
                 uint32_t r[128];
 #pragma unroll
@@ -180,7 +158,7 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
                 bool waited = !S::APART || j == 0;
                 auto wait_pv = [&] {
                     if (!waited) {
-                        if (!mbar_try_wait(pv_done + w, (n_s - 1) & 1)) ok = mbar_wait(pv_done + w, (n_s - 1) & 1, POLL_LIMIT) && ok;
+                        wait_for(pv_done + w, (n_s - 1) & 1, ok);
                         tc_fence_after_sync();
                         waited = true;
                     }
@@ -206,8 +184,7 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
                 // Turns at the exponentials: 2 x 4133 x 4096, 37 heads of 128, 755 -> 690 us.  (With P apart, where nothing else waits
                 // for products, the hand-over costs more than it gives: 468 -> 519 us at 64.)
                 if (!S::APART && x.both) {
-                    if ((w || n_turn) && !mbar_try_wait(turn + warp, (w ? n_turn : n_turn - 1) & 1))
-                        ok = mbar_wait(turn + warp, (w ? n_turn : n_turn - 1) & 1, POLL_LIMIT) && ok;
+                    if (w || n_turn) wait_for(turn + warp, (w ? n_turn : n_turn - 1) & 1, ok);
                     ++n_turn;
                 }
                 const float ref = m == -INFINITY ? 0.f : m * c;
@@ -412,19 +389,6 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
     __syncthreads();
     tc_fence_after_sync();
     if (warp == 9) tmem_dealloc(tmem, 512);
-}
-
-// [B, tokens, heads, D] with `stride` elements from token to token; box: BOX channels x heads x tokens of one image
-bool rows_map(CUtensorMap* m, const void* base, int D, int heads, long long tokens, int B, long long stride, int box_ch, int box_heads, int box_tokens) {
-    EncodeTiledFn enc = tma_encoder();
-    if (!enc) return false;
-    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)tokens, (cuuint64_t)B};
-    const cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2, (cuuint64_t)(stride * tokens) * 2};
-    const cuuint32_t box[4] = {(cuuint32_t)box_ch, (cuuint32_t)box_heads, (cuuint32_t)box_tokens, 1};
-    const cuuint32_t es[4] = {1, 1, 1, 1};
-    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               box_ch == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int D>

@@ -1,0 +1,533 @@
+// Gradients of cross attention, bf16, on the 5th-generation tensor cores: many rows, many keys.  With P = 2^(scale log2e Q K^T - lse2),
+// dP = dO V^T, delta = rowsum(dO o O), dS = P o (dP - delta):  dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO.
+//
+// Two kernels of one form, each sum with one owner and a fixed order: one keeps a tile of 128 query rows (Q, dO) and walks blocks of 128
+// keys (dQ), the other keeps 128 keys (K, V) and walks blocks of query rows of all heads of its group (dK, dV).  X1, X2 are the kept tiles,
+// Y1, Y2 the walked ones:
+//   S = X1 Y1^T, dP = X2 Y2^T (128 x 128, fp32 in tensor memory),  A1 += dS Y1,  (dK, dV) A2 += P Y2,  dS and P read from tensor memory.
+// A one-kernel form with atomics on dQ would need five products instead of seven; its sums would depend on the order of arrival.
+//
+// One CTA per SM walks tiles; two warpgroups share the 128 lanes of a tile, 64 columns each: a thread turns 64 scores into P and 64 values of
+// dP into dS, and needs nothing from its neighbours (lse and delta are known).  Warp 8 copies (bulk tensor copies through a ring), warp 9
+// issues the products, warp 10 zeroes hidden keys' rows.  S and dP of the next block are made as soon as this one's are in registers, where P
+// and dS have tensor memory of their own; at head dim 128 the four accumulators of dK, dV fill it, P lies over S and dS over dP.
+// Per block the products are 1100 (dQ) and 1670 (dK, dV) cycles of the tensor pipe at head dim 64, 1560 and 2080 at 128; the
+// exponentials 1024 of the MUFU; what bounds it is the chain from S over P to dS at two warps a scheduler.
+//
+// Rounding: P and dS to bf16 for the products that contract over them (half a step, 2^-8, per term); everything else is fp32.
+#include "cross_tc_common.cuh"
+
+#include <math.h>
+
+namespace bra {
+namespace {
+
+using namespace cross_tc;
+
+constexpr int THREADS = 384;
+
+template <int D, bool DKV>
+struct Shape {
+    static constexpr int BOX = D < 64 ? D : 64, BOXES = D / BOX, ROW = BOX * 2, PLANE = 128 * ROW, TILE = PLANE * BOXES;
+    static constexpr int STAGES = D == 128 ? 2 : 4;
+    static constexpr uint32_t SWIZZLE = D < 64 ? 4 : 2;
+    static constexpr int STAGE = 2 * TILE;                          // Y1, Y2
+    static constexpr int OFF_Y = 2 * TILE, OFF_STAT = OFF_Y + STAGES * STAGE, OFF_BAR = OFF_STAT + (DKV ? STAGES * 1024 : 0);
+    static constexpr size_t smem = OFF_BAR + 256 + 1024;
+    // tensor memory: S 0, dP 128, A1 256, A2 behind it, P and dS behind both or over S and dP
+    static constexpr bool S_APART = !DKV || D <= 64, DS_APART = !DKV || D <= 64;
+    static constexpr int TM_DP = 128, TM_A1 = 256, TM_A2 = 256 + D;
+    static constexpr int TM_P = S_APART ? 384 : 0, TM_DS = DS_APART ? (D <= 64 ? 448 : 384) : TM_DP;
+    static constexpr int P_HALF = S_APART ? 32 : 64, DS_HALF = DS_APART ? 32 : 64;      // from the first warpgroup's columns to the second's
+};
+
+struct TcArgs {
+    CrossArgs a;
+    const float* stats;     // [pair][row block][2][128]: -log2 of the softmax denominator, -delta
+    int tokens;             // of a tile of rows: 128 / group
+    int row_blocks;         // of a pair
+    int tiles;              // kept tiles of a pair
+    int total;
+    FastDiv tiles_div;
+};
+
+template <int D, bool DKV>
+__global__ void __launch_bounds__(THREADS, 1)
+cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                     const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do) {
+    using S = Shape<D, DKV>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint64_t* bar = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR);
+    uint64_t *x_full = bar, *x_empty = bar + 1, *s_ready = bar + 2, *dp_ready = bar + 3, *s_free = bar + 4, *dp_free = bar + 5, *p_ready = bar + 6,
+             *ds_ready = bar + 7, *pv_done = bar + 8, *acc_done = bar + 9, *y_full = bar + 10, *y_clean = y_full + S::STAGES,
+             *y_empty = y_clean + S::STAGES;
+    uint32_t* slot = reinterpret_cast<uint32_t*>(y_empty + S::STAGES);
+    const uint32_t base = smem_u32(smem);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const CrossArgs& a = g.a;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 10; ++i) mbar_init(bar + i, i >= 4 && i <= 7 ? 256 : 1);
+        for (int s = 0; s < 3 * S::STAGES; ++s) mbar_init(y_full + s, 1);
+        fence_mbar_init();
+    }
+    // rows of a block that no copy writes (a group that does not divide 128) meet a P of zero: they must be finite
+    if (DKV && g.tokens * a.group < 128) {
+        for (int i = threadIdx.x; i < S::STAGES * S::STAGE / 16; i += THREADS) sts_f32x4(base + S::OFF_Y + i * 16, 0.f, 0.f, 0.f, 0.f);
+        fence_proxy_async_smem();
+    }
+    if (warp == 9) tmem_alloc(slot, 512);
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = *slot;
+    bool ok = true;
+    pdl_wait();                             // the statistics of the kernel before
+    pdl_launch_dependents();
+
+    // every role walks the same tiles
+    struct Tile { int p, b, kvh, x0, end, blocks; };         // x0: first token of the kept tile (a query's or a key)
+    auto tile_of = [&](int t) {
+        Tile x;
+        x.p = (int)fdiv((uint32_t)t, g.tiles_div);
+        x.x0 = (t - x.p * g.tiles) * (DKV ? 128 : g.tokens);
+        x.b = (int)fdiv((uint32_t)x.p, a.kv_div);
+        x.kvh = x.p - x.b * a.kv;
+        x.end = cross_key_end(a, x.b);
+        x.blocks = DKV ? (x.x0 < x.end ? g.row_blocks : 0) : (x.end + 127) >> 7;
+        return x;
+    };
+
+    // registers: launched with 168 a thread, 384 x 168 = 64512 = 256 x 224 + 128 x 56
+    if (warp < 8) {
+        // ------------------------------------------------ P and dS
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        const int half = warp >> 2, row = threadIdx.x & 127;
+        const uint32_t tl = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        const float c = a.scale_log2;
+        const float2 c2 = make_float2(c, c);
+        const int in_token = DKV ? 0 : (int)fdiv((uint32_t)row, a.group_div), head = DKV ? 0 : row - in_token * a.group;
+        uint32_t n = 0;                         // blocks so far
+        for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
+            const Tile x = tile_of(t);
+            const uint8_t* mask = a.key_mask ? a.key_mask + (long long)x.b * a.Nk : nullptr;
+            float nl = 0.f, nd = 0.f;           // -lse2, -delta of the thread's row (dQ)
+            if (!DKV) {
+                const float* st = g.stats + ((long long)x.p * g.row_blocks + x.x0 / g.tokens) * 256 + row;
+                nl = __ldcg(st);
+                nd = __ldcg(st + 128);
+            }
+            const float2 nl2 = make_float2(nl, nl), nd2 = make_float2(nd, nd);
+            uint32_t bytes = !DKV && mask ? mask_bytes(mask, 0, x.end, lane) : 0u;
+            for (int j = 0; j < x.blocks; ++j, ++n) {
+                const int stage = n % S::STAGES;
+                const uint32_t stat = base + S::OFF_STAT + stage * 1024 + half * 256;
+                const bool cut = !DKV && (mask || (j + 1) * 128 > x.end);        // some keys may be hidden
+                uint32_t see[2] = {0u, 0u};
+                if (cut) {
+                    const Seen seen = seen_of(mask, bytes, j * 128, x.end);
+                    see[0] = seen.w[2 * half];
+                    see[1] = seen.w[2 * half + 1];
+                    if (mask) bytes = mask_bytes(mask, (j + 1) * 128, x.end, lane);
+                }
+                if (DKV) wait_for(y_full + stage, (n / S::STAGES) & 1, ok);       // the rows' statistics
+                wait_for(s_ready, n & 1, ok);
+                tc_fence_after_sync();
+                uint32_t p[64];
+                tmem_ld_32x32b_x32(tl + half * 64, p);
+                tmem_ld_32x32b_x32(tl + half * 64 + 32, p + 32);
+                tmem_ld_wait();
+                if (S::S_APART) {
+                    tc_fence_before_sync();
+                    mbar_arrive(s_free);
+                }
+                auto pair = [](const uint32_t* r) { return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1])); };
+#pragma unroll
+                for (int k = 0; k < 64; k += 4) {
+                    float2 m0 = nl2, m1 = nl2;
+                    if (DKV) {
+                        const float4 v = lds_f32x4(stat + k * 4);
+                        m0 = make_float2(v.x, v.y);
+                        m1 = make_float2(v.z, v.w);
+                    }
+                    const float2 u = __ffma2_rn(pair(p + k), c2, m0), v = __ffma2_rn(pair(p + k + 2), c2, m1);
+                    p[k] = __float_as_uint(ex2_approx(u.x));
+                    p[k + 1] = __float_as_uint(ex2_approx(u.y));
+                    p[k + 2] = __float_as_uint(ex2_approx(v.x));
+                    p[k + 3] = __float_as_uint(ex2_approx(v.y));
+                }
+                if (DKV) {
+                    if (S::S_APART && j > 0) {
+                        wait_for(pv_done, (n - 1) & 1, ok);
+                        tc_fence_after_sync();
+                    }
+#pragma unroll
+                    for (int k = 0; k < 64; k += 32) {
+                        uint32_t q[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) q[e] = pack2_bf16(__uint_as_float(p[k + 2 * e]), __uint_as_float(p[k + 2 * e + 1]));
+                        tmem_st_32x32b_x16(tl + S::TM_P + half * S::P_HALF + k / 2, q);
+                    }
+                    tmem_st_wait();
+                    tc_fence_before_sync();
+                    mbar_arrive(p_ready);
+                }
+                wait_for(dp_ready, n & 1, ok);
+                tc_fence_after_sync();
+                uint32_t dp[64];
+                tmem_ld_32x32b_x32(tl + S::TM_DP + half * 64, dp);
+                tmem_ld_32x32b_x32(tl + S::TM_DP + half * 64 + 32, dp + 32);
+                tmem_ld_wait();
+                if (S::DS_APART) {
+                    tc_fence_before_sync();
+                    mbar_arrive(dp_free);
+                }
+#pragma unroll
+                for (int k = 0; k < 64; k += 4) {
+                    float2 m0 = nd2, m1 = nd2;
+                    if (DKV) {
+                        const float4 v = lds_f32x4(stat + 512 + k * 4);
+                        m0 = make_float2(v.x, v.y);
+                        m1 = make_float2(v.z, v.w);
+                    }
+                    const float2 u = __fmul2_rn(pair(p + k), __fadd2_rn(pair(dp + k), m0)), v = __fmul2_rn(pair(p + k + 2), __fadd2_rn(pair(dp + k + 2), m1));
+                    dp[k] = __float_as_uint(u.x);
+                    dp[k + 1] = __float_as_uint(u.y);
+                    dp[k + 2] = __float_as_uint(v.x);
+                    dp[k + 3] = __float_as_uint(v.y);
+                }
+                if (cut) {
+#pragma unroll
+                    for (int k = 0; k < 64; ++k)
+                        if (!((see[k >> 5] >> (k & 31)) & 1)) dp[k] = 0u;
+                }
+                if (S::DS_APART && j > 0) {
+                    wait_for(acc_done, (n - 1) & 1, ok);
+                    tc_fence_after_sync();
+                }
+#pragma unroll
+                for (int k = 0; k < 64; k += 32) {
+                    uint32_t q[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) q[e] = pack2_bf16(__uint_as_float(dp[k + 2 * e]), __uint_as_float(dp[k + 2 * e + 1]));
+                    tmem_st_32x32b_x16(tl + S::TM_DS + half * S::DS_HALF + k / 2, q);
+                }
+                tmem_st_wait();
+                tc_fence_before_sync();
+                mbar_arrive(ds_ready);
+                if (!ok) break;
+            }
+            if (!ok) break;
+            if (x.blocks) {
+                wait_for(acc_done, (n - 1) & 1, ok);
+                tc_fence_after_sync();
+            }
+            if (DKV) {
+                // one warpgroup stores dK, the other dV; thread = key
+                const int key = x.x0 + row;
+                bool live = key < x.end;
+                if (live && mask) live = __ldg(mask + key) != 0;
+                const bool have = key < a.Nk && ok;
+                const float f = half ? 1.f : a.scale;
+                __nv_bfloat16* out = half ? static_cast<__nv_bfloat16*>(a.dV) + ((long long)x.b * a.Nk + key) * a.v_stride
+                                          : static_cast<__nv_bfloat16*>(a.dK) + ((long long)x.b * a.Nk + key) * a.k_stride;
+                out += (long long)x.kvh * D;
+#pragma unroll
+                for (int k = 0; k < D; k += 32) {
+                    uint32_t o[32];
+                    if (x.blocks) {
+                        tmem_ld_32x32b_x32(tl + (half ? S::TM_A2 : S::TM_A1) + k, o);
+                        tmem_ld_wait();
+                    }
+                    if (have) {
+#pragma unroll
+                        for (int q = 0; q < 32; q += 8) {
+                            uint32_t v[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                v[e] = live && x.blocks ? pack2_bf16(__uint_as_float(o[q + 2 * e]) * f, __uint_as_float(o[q + 2 * e + 1]) * f) : 0u;
+                            *reinterpret_cast<uint4*>(out + k + q) = make_uint4(v[0], v[1], v[2], v[3]);
+                        }
+                    }
+                }
+            } else {
+                // half of the row's channels each
+                const int token = x.x0 + in_token;
+                const bool have = in_token < g.tokens && token < a.Nq && ok;
+                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.dQ) + ((long long)x.b * a.Nq + token) * a.q_stride +
+                                     (long long)(x.kvh * a.group + head) * D + half * (D / 2);
+#pragma unroll
+                for (int k = 0; k < D / 2; k += 16) {
+                    uint32_t o[16];
+                    if (x.blocks) {
+                        tmem_ld_32x32b_x16(tl + S::TM_A1 + half * (D / 2) + k, o);
+                        tmem_ld_wait();
+                    }
+                    if (have) {
+#pragma unroll
+                        for (int q = 0; q < 16; q += 8) {
+                            uint32_t v[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                v[e] = x.blocks ? pack2_bf16(__uint_as_float(o[q + 2 * e]) * a.scale, __uint_as_float(o[q + 2 * e + 1]) * a.scale) : 0u;
+                            *reinterpret_cast<uint4*>(out + k + q) = make_uint4(v[0], v[1], v[2], v[3]);
+                        }
+                    }
+                }
+            }
+            tc_fence_before_sync();
+        }
+    } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == 8) {
+        // ------------------------------------------------ copies
+        if (lane == 0) {
+            uint32_t n_x = 0, n = 0;
+            const uint32_t rows_box = (uint32_t)(g.tokens * a.group * S::ROW), keys_box = S::PLANE;
+            for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
+                const Tile x = tile_of(t);
+                if (!x.blocks) continue;
+                if (n_x) ok = mbar_wait(x_empty, (n_x - 1) & 1, POLL_LIMIT) && ok;
+                ++n_x;
+                if (!ok) break;
+                mbar_expect_tx(x_full, 2 * S::BOXES * (DKV ? keys_box : rows_box));
+#pragma unroll
+                for (int k = 0; k < S::BOXES; ++k) {
+                    const uint32_t to = base + k * S::PLANE;
+                    tma_load_4d(to, DKV ? &map_k : &map_q, x_full, k * S::BOX, DKV ? x.kvh : x.kvh * a.group, x.x0, x.b);
+                    tma_load_4d(to + S::TILE, DKV ? &map_v : &map_do, x_full, k * S::BOX, DKV ? x.kvh : x.kvh * a.group, x.x0, x.b);
+                }
+                for (int j = 0; j < x.blocks && ok; ++j, ++n) {
+                    const int s = n % S::STAGES;
+                    if (n >= S::STAGES) ok = mbar_wait(y_empty + s, (n / S::STAGES - 1) & 1, POLL_LIMIT) && ok;
+                    if (!ok) break;
+                    mbar_expect_tx(y_full + s, 2 * S::BOXES * (DKV ? rows_box : keys_box) + (DKV ? 1024 : 0));
+                    const int y0 = j * (DKV ? g.tokens : 128);
+#pragma unroll
+                    for (int k = 0; k < S::BOXES; ++k) {
+                        const uint32_t to = base + S::OFF_Y + s * S::STAGE + k * S::PLANE;
+                        tma_load_4d(to, DKV ? &map_q : &map_k, y_full + s, k * S::BOX, DKV ? x.kvh * a.group : x.kvh, y0, x.b);
+                        tma_load_4d(to + S::TILE, DKV ? &map_do : &map_v, y_full + s, k * S::BOX, DKV ? x.kvh * a.group : x.kvh, y0, x.b);
+                    }
+                    if (DKV) bulk_load(base + S::OFF_STAT + s * 1024, g.stats + ((long long)x.p * g.row_blocks + j) * 256, 1024, y_full + s);
+                }
+            }
+        }
+    } else if (warp == 9) {
+        // ------------------------------------------------ products
+        constexpr uint32_t IDESC_S = umma_idesc_bf16(128, 128, false, false), IDESC_A = umma_idesc_bf16(128, D, false, true);
+        uint32_t n_x = 0, n = 0;                    // tiles with a walk, blocks so far
+        // S (which = 0) or dP (1) of block i
+        auto scores = [&](uint32_t i, int which) {
+            const int s = i % S::STAGES;
+            ok = mbar_wait(y_full + s, (i / S::STAGES) & 1, POLL_LIMIT) && ok;
+            if (!ok) return;
+            tc_fence_after_sync();
+            if (lane == 0) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    const uint32_t at = (uint32_t)(which * S::TILE + k * 16 / S::BOX * S::PLANE + k * 16 % S::BOX * 2);
+                    umma_ss(tmem + which * S::TM_DP, umma_smem_desc(base + at, 16, 8 * S::ROW, S::SWIZZLE),
+                            umma_smem_desc(base + S::OFF_Y + s * S::STAGE + at, 16, 8 * S::ROW, S::SWIZZLE), IDESC_S, k);
+                }
+                umma_commit(which ? dp_ready : s_ready);
+            }
+        };
+        // A1 += dS Y1 (which = 0), A2 += P Y2 (1), of block i
+        auto gather = [&](uint32_t i, int which, bool first) {
+            tc_fence_after_sync();
+            if (lane == 0) {
+                const uint32_t y = base + S::OFF_Y + (i % S::STAGES) * S::STAGE + which * S::TILE;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {               // 16 walked rows
+                    const uint32_t from = which ? S::TM_P + (k >> 2) * S::P_HALF + (k & 3) * 8 : S::TM_DS + (k >> 2) * S::DS_HALF + (k & 3) * 8;
+                    umma_ts(tmem + (which ? S::TM_A2 : S::TM_A1), tmem + from,
+                            umma_smem_desc(y + k * 16 * S::ROW, S::BOXES > 1 ? S::PLANE : 16, 8 * S::ROW, S::SWIZZLE), IDESC_A, !first || k > 0);
+                }
+            }
+        };
+        for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
+            const Tile x = tile_of(t);
+            if (!x.blocks) continue;
+            ok = mbar_wait(x_full, n_x & 1, POLL_LIMIT) && ok;
+            ++n_x;
+            if (ok) scores(n, 0);
+            if (ok) scores(n, 1);
+            if (lane == 0 && x.blocks == 1) umma_commit(x_empty);
+            for (int j = 0; j < x.blocks && ok; ++j, ++n) {
+                const bool more = j + 1 < x.blocks;
+                if (S::S_APART) {
+                    ok = mbar_wait(s_free, n & 1, POLL_LIMIT) && ok;
+                    if (more && ok) scores(n + 1, 0);
+                    if (!ok) break;
+                }
+                if (DKV) {
+                    ok = mbar_wait(p_ready, n & 1, POLL_LIMIT) && ok;
+                    if (!ok) break;
+                    gather(n, 1, j == 0);
+                    if (S::S_APART) {
+                        if (lane == 0) umma_commit(pv_done);
+                    } else if (more) {
+                        scores(n + 1, 0);
+                        if (!ok) break;
+                    }
+                }
+                if (S::DS_APART) {
+                    ok = mbar_wait(dp_free, n & 1, POLL_LIMIT) && ok;
+                    if (more && ok) scores(n + 1, 1);
+                    if (!ok) break;
+                    if (lane == 0 && j + 2 == x.blocks) umma_commit(x_empty);
+                }
+                if (!DKV) ok = mbar_wait(y_clean + n % S::STAGES, (n / S::STAGES) & 1, POLL_LIMIT) && ok;
+                ok = mbar_wait(ds_ready, n & 1, POLL_LIMIT) && ok;
+                if (!ok) break;
+                gather(n, 0, j == 0);
+                if (lane == 0) {
+                    umma_commit(acc_done);
+                    umma_commit(y_empty + n % S::STAGES);
+                }
+                if (!S::DS_APART && more) {
+                    scores(n + 1, 1);
+                    if (!ok) break;
+                    if (lane == 0 && j + 2 == x.blocks) umma_commit(x_empty);
+                }
+            }
+        }
+    } else if (warp == 10 && !DKV) {
+        // ------------------------------------------------ rows of hidden keys, before dS (zero there) meets them
+        uint32_t n = 0;
+        for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
+            const Tile x = tile_of(t);
+            const uint8_t* mask = a.key_mask ? a.key_mask + (long long)x.b * a.Nk : nullptr;
+            for (int j = 0; j < x.blocks && ok; ++j, ++n) {
+                const int s = n % S::STAGES;
+                const Seen seen = seen_of(mask, mask ? mask_bytes(mask, j * 128, x.end, lane) : 0u, j * 128, x.end);
+                ok = mbar_wait(y_full + s, (n / S::STAGES) & 1, POLL_LIMIT) && ok;
+                if ((seen.w[0] & seen.w[1] & seen.w[2] & seen.w[3]) != 0xffffffffu) {
+                    constexpr int CHUNKS = S::ROW / 16;
+                    for (int r = lane / CHUNKS; r < 128; r += 32 / CHUNKS)
+                        if (!((seen.w[r >> 5] >> (r & 31)) & 1)) {
+#pragma unroll
+                            for (int k = 0; k < S::BOXES; ++k)
+                                sts_f32x4(base + S::OFF_Y + s * S::STAGE + k * S::PLANE + r * S::ROW + lane % CHUNKS * 16, 0.f, 0.f, 0.f, 0.f);
+                        }
+                    fence_proxy_async_smem();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(y_clean + s);
+            }
+        }
+    }
+    }
+    __syncwarp();
+    if (!ok) record_error(a.status, BRA_ERR_TIMEOUT, (int)blockIdx.x);
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    if (warp == 9) tmem_dealloc(tmem, 512);
+}
+
+// (-lse2, -delta) of every row, by blocks of 128 as the kernels above walk them; rows that do not exist and rows that see no key:
+// (-inf, 0), so that every P of theirs is zero.  D / 8 lanes a row, 16 bytes each of O and dO.
+template <int D>
+__global__ void __launch_bounds__(256) cross_stats_kernel(const TcArgs g, float* stats) {
+    constexpr int LANES = D / 8;
+    const CrossArgs& a = g.a;
+    pdl_launch_dependents();
+    const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) / LANES;
+    const int part = threadIdx.x % LANES;
+    const long long block = i >> 7;
+    const int row = (int)(i & 127);
+    const int p = (int)(block / g.row_blocks), j = (int)(block - (long long)p * g.row_blocks);
+    const int b = (int)fdiv((uint32_t)p, a.kv_div), kvh = p - b * a.kv;
+    const int in_token = (int)fdiv((uint32_t)row, a.group_div), h = kvh * a.group + row - in_token * a.group;
+    const int token = j * g.tokens + in_token;
+    const bool have = p < g.total && in_token < g.tokens && token < a.Nq;      // total: pairs here
+    float delta = 0.f;
+    if (have) {
+        const long long off = ((long long)b * a.Nq + token) * a.o_stride + (long long)h * D + part * 8;
+        float o[8], d[8];
+        load_row<8>(static_cast<const __nv_bfloat16*>(a.O) + off, o);
+        load_row<8>(static_cast<const __nv_bfloat16*>(a.dO) + off, d);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) delta = fmaf(o[e], d[e], delta);
+    }
+#pragma unroll
+    for (int x = LANES / 2; x; x >>= 1) delta += __shfl_xor_sync(0xffffffffu, delta, x);
+    if (part == 0 && p < g.total) {
+        float l = -INFINITY;
+        if (have) {
+            const float e = __ldg(a.lse + ((long long)b * a.heads + h) * a.Nq + token);
+            if (e != -INFINITY) l = -e * 1.4426950408889634f;
+        }
+        stats[block * 256 + row] = l;
+        stats[block * 256 + 128 + row] = l == -INFINITY ? 0.f : -delta;
+    }
+}
+
+int row_blocks(const CrossDims& d) { return (d.Nq + 128 / d.group - 1) / (128 / d.group); }
+
+template <int D>
+cudaError_t launch(const CrossDims& d, const CrossArgs& a, cudaStream_t st) {
+    TcArgs g;
+    g.a = a;
+    float* stats = reinterpret_cast<float*>(a.stats);
+    g.stats = stats;
+    g.tokens = 128 / d.group;
+    g.row_blocks = row_blocks(d);
+    const int pairs = d.B * d.kv;
+    constexpr int BOX = D < 64 ? D : 64;
+    CUtensorMap q, k, v, o;
+    if (!rows_map(&q, a.Q, D, d.heads, d.Nq, d.B, d.q_stride, BOX, d.group, g.tokens) || !rows_map(&k, a.K, D, d.kv, d.Nk, d.B, d.k_stride, BOX, 1, 128) ||
+        !rows_map(&v, a.V, D, d.kv, d.Nk, d.B, d.v_stride, BOX, 1, 128) || !rows_map(&o, a.dO, D, d.heads, d.Nq, d.B, d.o_stride, BOX, d.group, g.tokens))
+        return cudaErrorInvalidValue;
+    static PerDeviceOnce attr;
+    cudaError_t e = attr.run([&] {
+        const cudaError_t f = cudaFuncSetAttribute(cross_grad_tc_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<D, false>::smem);
+        return f != cudaSuccess ? f : cudaFuncSetAttribute(cross_grad_tc_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<D, true>::smem);
+    });
+    if (e != cudaSuccess) return e;
+    g.tiles = 1;
+    g.total = pairs;
+    const long long lanes = (long long)pairs * g.row_blocks * 128 * (D / 8);
+    cross_stats_kernel<D><<<(unsigned)((lanes + 255) / 256), 256, 0, st>>>(g, stats);
+    count_launch();
+    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    g.tiles = g.row_blocks;
+    g.total = pairs * g.tiles;
+    g.tiles_div = fast_div(g.tiles);
+    e = launch_kernel(cross_grad_tc_kernel<D, false>, dim3(g.total < kSMs ? g.total : kSMs), dim3(THREADS), Shape<D, false>::smem, st, true, g, q, k, v, o);
+    if (e != cudaSuccess) return e;
+    count_launch();
+    g.tiles = (d.Nk + 127) / 128;
+    g.total = pairs * g.tiles;
+    g.tiles_div = fast_div(g.tiles);
+    e = launch_kernel(cross_grad_tc_kernel<D, true>, dim3(g.total < kSMs ? g.total : kSMs), dim3(THREADS), Shape<D, true>::smem, st, true, g, q, k, v, o);
+    if (e != cudaSuccess) return e;
+    count_launch();
+    return cudaSuccess;
+}
+
+}  // namespace
+
+size_t cross_backward_tc_stats(const CrossDims& d) { return sizeof(float) * 256 * (size_t)d.B * d.kv * row_blocks(d); }
+
+bool cross_backward_tc_pays(const CrossDims& d) {
+    if (d.D < 32 || d.group > 128 || d.esize != 2) return false;
+    const long long pairs = (long long)d.B * d.kv;
+    if (pairs * row_blocks(d) > (1 << 24) || pairs * ((d.Nk + 127) / 128) > (1 << 30)) return false;
+    static const char* force = getenv("BRA_TC");
+    if (force) return force[0] == '1';
+    return d.rows >= 128 && d.Nk >= 128;
+}
+
+cudaError_t launch_cross_backward_tc(const CrossDims& d, CrossArgs a, cudaStream_t st) {
+    switch (d.D) {
+        case 32: return launch<32>(d, a, st);
+        case 64: return launch<64>(d, a, st);
+        default: return launch<128>(d, a, st);
+    }
+}
+
+}  // namespace bra

@@ -29,7 +29,7 @@ struct CrossArgs {
     float* lse;
     const int32_t* key_len;
     const uint8_t* key_mask;
-    float2* stats;                                  // [B * kv][rows, padded to 64]: log2 of the softmax denominator, delta
+    float2* stats;                                  // of the rows: log2 of the softmax denominator, delta (layout: the kernels' own)
     float* part;                                    // fp32 sums of split work
     int32_t* done;
     int32_t* status;                                // error words (bra_device_status)
@@ -59,6 +59,9 @@ cudaError_t launch_cross_attend_mma(const CrossDims& d, CrossArgs a, cudaStream_
 bool cross_attend_tc_pays(const CrossDims& d);
 cudaError_t launch_cross_attend_tc(const CrossDims& d, CrossArgs a, cudaStream_t st);
 cudaError_t launch_cross_backward_mma(const CrossDims& d, CrossArgs a, cudaStream_t st);
+bool cross_backward_tc_pays(const CrossDims& d);
+size_t cross_backward_tc_stats(const CrossDims& d);         // bytes of its rows' statistics
+cudaError_t launch_cross_backward_tc(const CrossDims& d, CrossArgs a, cudaStream_t st);
 cudaError_t launch_cross_attend_simt(const CrossDims& d, CrossArgs a, cudaStream_t st);
 cudaError_t launch_cross_backward_simt(const CrossDims& d, CrossArgs a, cudaStream_t st);
 size_t cross_attend_mma_part(const CrossDims& d);

@@ -1,0 +1,53 @@
+// Cross attention on the 5th-generation tensor cores: what the forward and backward kernels share.
+#pragma once
+
+#include "cross_common.cuh"
+#include "tma_map.h"
+
+namespace bra {
+namespace cross_tc {
+
+using namespace ptx;
+
+constexpr uint32_t POLL_LIMIT = 4000000u;
+
+// Which of the 128 keys from key0 on are seen, 32 a word, the same in all lanes of a warp.
+struct Seen { uint32_t w[4]; };
+__device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+// the mask's bytes of a lane (one of each word), read a block ahead of their use
+__device__ __forceinline__ uint32_t mask_bytes(const uint8_t* mask, int key0, int end, int lane) {
+    uint32_t v = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const int j = key0 + 32 * w + lane;
+        if (j < end && __ldg(mask + j)) v |= 1u << w;
+    }
+    return v;
+}
+__device__ __forceinline__ Seen seen_of(const uint8_t* mask, uint32_t bytes, int key0, int end) {
+    Seen s;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) s.w[w] = mask ? __ballot_sync(0xffffffffu, (bytes >> w) & 1) : below(end - key0 - 32 * w);
+    return s;
+}
+
+// one attempt first: the loop around further ones costs a hundred cycles even where it is not needed
+__device__ __forceinline__ void wait_for(uint64_t* bar, uint32_t parity, bool& ok) {
+    if (!mbar_try_wait(bar, parity)) ok = mbar_wait(bar, parity, POLL_LIMIT) && ok;
+}
+
+// [B, tokens, heads, D] with `stride` elements from token to token; box: BOX channels x heads x tokens of one image
+inline bool rows_map(CUtensorMap* m, const void* base, int D, int heads, long long tokens, int B, long long stride, int box_ch, int box_heads, int box_tokens) {
+    EncodeTiledFn enc = tma_encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)tokens, (cuuint64_t)B};
+    const cuuint64_t strides[3] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2, (cuuint64_t)(stride * tokens) * 2};
+    const cuuint32_t box[4] = {(cuuint32_t)box_ch, (cuuint32_t)box_heads, (cuuint32_t)box_tokens, 1};
+    const cuuint32_t es[4] = {1, 1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               box_ch == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace cross_tc
+}  // namespace bra
