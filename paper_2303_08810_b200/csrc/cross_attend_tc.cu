@@ -291,17 +291,21 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
         // The second tile's warp follows the ring through pairs that have only one, without products: a wait two phases ahead of a
         // barrier would not be one.
         bool idle = false;
+        const uint64_t q_desc = umma_smem_desc(base + w * S::TILE, 16, 8 * S::ROW, S::SWIZZLE);
+        const uint64_t k_desc = umma_smem_desc(base + S::OFF_K, 16, 8 * S::ROW, S::SWIZZLE);
+        const uint64_t v_desc = umma_smem_desc(base + S::OFF_V, S::BOXES > 1 ? S::PLANE : 16, 8 * S::ROW, S::SWIZZLE);
         auto scores = [&] {
             const int stage = nk % S::STAGES;
-            ok = mbar_wait(k_full + stage, (nk / S::STAGES) & 1, POLL_LIMIT) && ok;
+            wait_for(k_full + stage, (nk / S::STAGES) & 1, ok);
             if (!ok) return;
             tc_fence_after_sync();
-            if (lane == 0 && !idle) {
+            if (!idle) {
+                const uint64_t kd = k_desc + stage * (S::TILE >> 4);
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t at = (uint32_t)(k * 16 / S::BOX * S::PLANE + k * 16 % S::BOX * 2);
-                    umma_ss(tmem + w * 128, umma_smem_desc(base + w * S::TILE + at, 16, 8 * S::ROW, S::SWIZZLE),
-                            umma_smem_desc(base + S::OFF_K + stage * S::TILE + at, 16, 8 * S::ROW, S::SWIZZLE), IDESC_S, k);
+                    constexpr int PER = S::BOX / 16;
+                    const uint32_t at = (uint32_t)(k / PER * S::PLANE + k % PER * 32) >> 4;
+                    umma_ss(tmem + w * 128, q_desc + at, kd + at, IDESC_S, k);
                 }
                 umma_commit(s_ready + w);
             }
@@ -309,16 +313,15 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
         };
         // stages are given back by both warps
         auto after_scores = [&](const Tile& x, int j) {
-            if (lane == 0) {
-                umma_commit(k_empty + (nk - 1) % S::STAGES);
-                if (j + 1 == x.blocks) umma_commit(q_empty);
-            }
+            umma_commit(k_empty + (nk - 1) % S::STAGES);
+            if (j + 1 == x.blocks) umma_commit(q_empty);
         };
-        for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
+        // One lane alone: lanes that only waited along could fall two phases behind a barrier, whose parity then says nothing.
+        for (int t = blockIdx.x; lane == 0 && t < g.total && ok; t += gridDim.x) {
             const Tile x = tile_of(t);
             if (!x.blocks) continue;
             idle = w && !x.both;
-            ok = mbar_wait(q_full, n_q & 1, POLL_LIMIT) && ok;
+            wait_for(q_full, n_q & 1, ok);
             ++n_q;
             if (!ok) break;
             scores();
@@ -328,26 +331,23 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
                 const int sv = nv % S::STAGES;
                 const bool more = j + 1 < x.blocks;
                 if (S::APART && more) {                         // S of this block is in registers
-                    if (!idle) ok = mbar_wait(s_free + w, nb & 1, POLL_LIMIT) && ok;
+                    if (!idle) wait_for(s_free + w, nb & 1, ok);
                     if (ok) scores();
                     if (!ok) break;
                     after_scores(x, j + 1);
                 }
-                ok = mbar_wait(v_clean + sv, (nv / S::STAGES) & 1, POLL_LIMIT) && ok;
-                if (!idle) ok = mbar_wait(p_ready + w, nb & 1, POLL_LIMIT) && ok;
+                wait_for(v_clean + sv, (nv / S::STAGES) & 1, ok);
+                if (!idle) wait_for(p_ready + w, nb & 1, ok);
                 if (!ok) break;
                 tc_fence_after_sync();
-                if (lane == 0 && !idle) {
+                if (!idle) {
+                    const uint64_t vd = v_desc + sv * (S::TILE >> 4);
 #pragma unroll
                     for (int k = 0; k < 8; ++k)                 // 16 keys: 8 columns of P, 16 rows of V
-                        umma_ts(tmem + S::TM_O + w * S::O_STEP, tmem + S::TM_P + w * S::P_STEP + k * 8,
-                                umma_smem_desc(base + S::OFF_V + sv * S::TILE + k * 16 * S::ROW, S::BOXES > 1 ? S::PLANE : 16, 8 * S::ROW, S::SWIZZLE),
-                                IDESC_O, j > 0 || k > 0);
+                        umma_ts(tmem + S::TM_O + w * S::O_STEP, tmem + S::TM_P + w * S::P_STEP + k * 8, vd + k * (16 * S::ROW >> 4), IDESC_O, j > 0 || k > 0);
                 }
-                if (lane == 0) {
-                    if (!idle) umma_commit(pv_done + w);
-                    umma_commit(v_empty + sv);
-                }
+                if (!idle) umma_commit(pv_done + w);
+                umma_commit(v_empty + sv);
                 if (!S::APART && more) {
                     scores();
                     if (!ok) break;

@@ -8,8 +8,8 @@
 // A one-kernel form with atomics on dQ would need five products instead of seven; its sums would depend on the order of arrival.
 //
 // One CTA per SM walks tiles; two warpgroups share the 128 lanes of a tile, 64 columns each: a thread turns 64 scores into P and 64 values of
-// dP into dS, and needs nothing from its neighbours (lse and delta are known).  Warp 8 copies (bulk tensor copies through a ring), warp 9
-// issues the products, warp 10 zeroes hidden keys' rows.  S and dP of the next block are made as soon as this one's are in registers, where P
+// dP into dS, and needs nothing from its neighbours (lse and delta are known).  Warp 8 copies (bulk tensor copies through a ring), warps 9 and
+// 10 issue the products, warp 11 zeroes hidden keys' rows.  S and dP of the next block are made as soon as this one's are in registers, where P
 // and dS have tensor memory of their own; at head dim 128 the four accumulators of dK, dV fill it, P lies over S and dS over dP.
 // Per block the products are 1100 (dQ) and 1670 (dK, dV) cycles of the tensor pipe at head dim 64, 1560 and 2080 at 128; the
 // exponentials 1024 of the MUFU; what bounds it is the chain from S over P to dS at two warps a scheduler.
@@ -68,8 +68,8 @@ cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, 
     const CrossArgs& a = g.a;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 10; ++i) mbar_init(bar + i, i >= 4 && i <= 7 ? 256 : 1);
-        for (int s = 0; s < 3 * S::STAGES; ++s) mbar_init(y_full + s, 1);
+        for (int i = 0; i < 10; ++i) mbar_init(bar + i, i == 1 ? 2 : i >= 4 && i <= 7 ? 256 : 1);
+        for (int s = 0; s < S::STAGES; ++s) { mbar_init(y_full + s, 1); mbar_init(y_clean + s, 1); mbar_init(y_empty + s, 2); }
         fence_mbar_init();
     }
     // rows of a block that no copy writes (a group that does not divide 128) meet a P of zero: they must be finite
@@ -221,6 +221,7 @@ cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, 
             if (!ok) break;
             if (x.blocks) {
                 wait_for(acc_done, (n - 1) & 1, ok);
+                if (DKV) wait_for(pv_done, (n - 1) & 1, ok);
                 tc_fence_after_sync();
             }
             if (DKV) {
@@ -314,87 +315,70 @@ cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, 
                 }
             }
         }
-    } else if (warp == 9) {
-        // ------------------------------------------------ products
+    } else if (warp < 11) {
+        // ------------------------------------------------ products: warp 9 makes S and A2, warp 10 dP and A1
+        // An issuing lane is held as long as its products run, and by every wait and commit besides: with one warp for all four
+        // the tensor pipe stood still for the 1100 cycles of those (of 2800 a block at head dim 64).
         constexpr uint32_t IDESC_S = umma_idesc_bf16(128, 128, false, false), IDESC_A = umma_idesc_bf16(128, D, false, true);
+        const int which = warp - 9;                 // 0: X1, Y1 make S; 1: X2, Y2 make dP
+        uint64_t *made = which ? dp_ready : s_ready, *taken = which ? dp_free : s_free, *given = which ? ds_ready : p_ready;
+        constexpr bool APART = S::S_APART;          // the same for both
+        static_assert(S::S_APART == S::DS_APART, "S and dP");
+        const uint64_t x_desc = umma_smem_desc(base + which * S::TILE, 16, 8 * S::ROW, S::SWIZZLE);
+        const uint64_t y_desc = umma_smem_desc(base + S::OFF_Y + which * S::TILE, 16, 8 * S::ROW, S::SWIZZLE);
+        // dS meets Y1, P meets Y2
+        const uint64_t z_desc = umma_smem_desc(base + S::OFF_Y + (which ^ 1) * S::TILE, S::BOXES > 1 ? S::PLANE : 16, 8 * S::ROW, S::SWIZZLE);
+        const uint32_t to = tmem + (which ? S::TM_A1 : S::TM_A2), from = tmem + (which ? S::TM_DS : S::TM_P);
+        constexpr int HALF = APART ? 32 : 64;
+        static_assert(S::P_HALF == HALF && S::DS_HALF == HALF, "halves of P and dS");
+        const bool gathers = DKV || which;
         uint32_t n_x = 0, n = 0;                    // tiles with a walk, blocks so far
-        // S (which = 0) or dP (1) of block i
-        auto scores = [&](uint32_t i, int which) {
-            const int s = i % S::STAGES;
-            ok = mbar_wait(y_full + s, (i / S::STAGES) & 1, POLL_LIMIT) && ok;
+        auto scores = [&](uint32_t i, bool last) {
+            const uint32_t s = i % S::STAGES;
+            wait_for(y_full + s, (i / S::STAGES) & 1, ok);
             if (!ok) return;
             tc_fence_after_sync();
-            if (lane == 0) {
+            const uint64_t y = y_desc + s * (S::STAGE >> 4);
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t at = (uint32_t)(which * S::TILE + k * 16 / S::BOX * S::PLANE + k * 16 % S::BOX * 2);
-                    umma_ss(tmem + which * S::TM_DP, umma_smem_desc(base + at, 16, 8 * S::ROW, S::SWIZZLE),
-                            umma_smem_desc(base + S::OFF_Y + s * S::STAGE + at, 16, 8 * S::ROW, S::SWIZZLE), IDESC_S, k);
-                }
-                umma_commit(which ? dp_ready : s_ready);
+            for (int k = 0; k < D / 16; ++k) {
+                constexpr int PER = S::BOX / 16;
+                const uint32_t at = (uint32_t)(k / PER * S::PLANE + k % PER * 32) >> 4;
+                umma_ss(tmem + which * S::TM_DP, x_desc + at, y + at, IDESC_S, k);
             }
+            umma_commit(made);
+            if (last) umma_commit(x_empty);
+            if (!gathers) umma_commit(y_empty + s);
         };
-        // A1 += dS Y1 (which = 0), A2 += P Y2 (1), of block i
-        auto gather = [&](uint32_t i, int which, bool first) {
-            tc_fence_after_sync();
-            if (lane == 0) {
-                const uint32_t y = base + S::OFF_Y + (i % S::STAGES) * S::STAGE + which * S::TILE;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {               // 16 walked rows
-                    const uint32_t from = which ? S::TM_P + (k >> 2) * S::P_HALF + (k & 3) * 8 : S::TM_DS + (k >> 2) * S::DS_HALF + (k & 3) * 8;
-                    umma_ts(tmem + (which ? S::TM_A2 : S::TM_A1), tmem + from,
-                            umma_smem_desc(y + k * 16 * S::ROW, S::BOXES > 1 ? S::PLANE : 16, 8 * S::ROW, S::SWIZZLE), IDESC_A, !first || k > 0);
-                }
-            }
-        };
-        for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
+        // One lane alone: lanes that only waited along could fall two phases behind a barrier, whose parity then says nothing.
+        for (int t = blockIdx.x; lane == 0 && t < g.total && ok; t += gridDim.x) {
             const Tile x = tile_of(t);
             if (!x.blocks) continue;
-            ok = mbar_wait(x_full, n_x & 1, POLL_LIMIT) && ok;
+            wait_for(x_full, n_x & 1, ok);
             ++n_x;
-            if (ok) scores(n, 0);
-            if (ok) scores(n, 1);
-            if (lane == 0 && x.blocks == 1) umma_commit(x_empty);
+            if (ok) scores(n, x.blocks == 1);
             for (int j = 0; j < x.blocks && ok; ++j, ++n) {
                 const bool more = j + 1 < x.blocks;
-                if (S::S_APART) {
-                    ok = mbar_wait(s_free, n & 1, POLL_LIMIT) && ok;
-                    if (more && ok) scores(n + 1, 0);
+                const uint32_t s = n % S::STAGES;
+                if (APART) {
+                    wait_for(taken, n & 1, ok);
+                    if (more && ok) scores(n + 1, j + 2 == x.blocks);
+                }
+                if (gathers) {
+                    if (!DKV) wait_for(y_clean + s, (n / S::STAGES) & 1, ok);
+                    wait_for(given, n & 1, ok);
                     if (!ok) break;
+                    tc_fence_after_sync();
+                    const uint64_t z = z_desc + s * (S::STAGE >> 4);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)                     // 16 walked rows
+                        umma_ts(to, from + (k >> 2) * HALF + (k & 3) * 8, z + k * (16 * S::ROW >> 4), IDESC_A, j > 0 || k > 0);
+                    umma_commit(which ? acc_done : pv_done);
+                    umma_commit(y_empty + s);
                 }
-                if (DKV) {
-                    ok = mbar_wait(p_ready, n & 1, POLL_LIMIT) && ok;
-                    if (!ok) break;
-                    gather(n, 1, j == 0);
-                    if (S::S_APART) {
-                        if (lane == 0) umma_commit(pv_done);
-                    } else if (more) {
-                        scores(n + 1, 0);
-                        if (!ok) break;
-                    }
-                }
-                if (S::DS_APART) {
-                    ok = mbar_wait(dp_free, n & 1, POLL_LIMIT) && ok;
-                    if (more && ok) scores(n + 1, 1);
-                    if (!ok) break;
-                    if (lane == 0 && j + 2 == x.blocks) umma_commit(x_empty);
-                }
-                if (!DKV) ok = mbar_wait(y_clean + n % S::STAGES, (n / S::STAGES) & 1, POLL_LIMIT) && ok;
-                ok = mbar_wait(ds_ready, n & 1, POLL_LIMIT) && ok;
-                if (!ok) break;
-                gather(n, 0, j == 0);
-                if (lane == 0) {
-                    umma_commit(acc_done);
-                    umma_commit(y_empty + n % S::STAGES);
-                }
-                if (!S::DS_APART && more) {
-                    scores(n + 1, 1);
-                    if (!ok) break;
-                    if (lane == 0 && j + 2 == x.blocks) umma_commit(x_empty);
-                }
+                if (!APART && more && ok) scores(n + 1, j + 2 == x.blocks);
             }
         }
-    } else if (warp == 10 && !DKV) {
+    } else if (!DKV) {
         // ------------------------------------------------ rows of hidden keys, before dS (zero there) meets them
         uint32_t n = 0;
         for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
