@@ -73,8 +73,8 @@ CrossWs cross_ws(const CrossDims& d) {
     L.done = off;  off += align256(sizeof(int32_t) * CROSS_COUNTERS);
     const size_t padded = sizeof(float2) * (size_t)d.B * d.kv * ((d.rows + 63) / 64 * 64), tc = cross_backward_tc_pays(d) ? cross_backward_tc_stats(d) : 0;
     L.stats = off; off += align256(padded > tc ? padded : tc);
-    const size_t f = d.esize == 2 ? cross_attend_mma_part(d) : cross_attend_simt_part(d);
-    const size_t b = d.esize == 2 ? cross_backward_mma_part(d) : cross_backward_simt_part(d);
+    const size_t f = d.esize != 2 ? cross_attend_simt_part(d) : cross_attend_tc_pays(d) ? cross_attend_tc_part(d) : cross_attend_mma_part(d);
+    const size_t b = d.esize != 2 ? cross_backward_simt_part(d) : cross_backward_tc_pays(d) ? cross_backward_tc_part(d) : cross_backward_mma_part(d);
     L.part = off;  off += align256(sizeof(float) * (f > b ? f : b));
     L.total = off;
     return L;

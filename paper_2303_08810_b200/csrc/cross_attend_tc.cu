@@ -51,11 +51,13 @@ struct TcArgs {
     CrossArgs a;
     int tokens;             // of a tile: 128 / group
     int pairs;              // tile pairs of an (image, key head)
-    int total;              // of all of them
-    FastDiv pairs_div;
+    int splits, part;       // parts of the walk over the keys and their length in blocks
+    int total;              // parts of all pairs
+    FastDiv pairs_div, splits_div;
 };
 
-template <int D>
+// SPLIT: walks are cut in parts
+template <int D, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
 cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                        const __grid_constant__ CUtensorMap map_v) {
@@ -91,15 +93,17 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
     bool ok = true;
 
     // every role walks the same tiles
-    struct Tile { int b, kvh, token0, end, blocks, both; };
+    struct Tile { int b, kvh, token0, end, j0, blocks, both; };
     auto tile_of = [&](int t) {
         Tile x;
-        const int p = (int)fdiv((uint32_t)t, g.pairs_div);
-        x.token0 = (t - p * g.pairs) * 2 * g.tokens;
+        const int pair = SPLIT ? (int)fdiv((uint32_t)t, g.splits_div) : t, p = (int)fdiv((uint32_t)pair, g.pairs_div);
+        x.j0 = SPLIT ? (t - pair * g.splits) * g.part : 0;
+        x.token0 = (pair - p * g.pairs) * 2 * g.tokens;
         x.b = (int)fdiv((uint32_t)p, a.kv_div);
         x.kvh = p - x.b * a.kv;
         x.end = cross_key_end(a, x.b);
         x.blocks = (x.end + 127) >> 7;
+        if (SPLIT) x.blocks = min(max(x.blocks - x.j0, 0), g.part);
         x.both = x.token0 + g.tokens < a.Nq;
         return x;
     };
@@ -122,13 +126,14 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
             const int token = x.token0 + w * g.tokens + in_token;
             const bool live = in_token < g.tokens && token < a.Nq;
             float m = -INFINITY, l = 0.f;
-            uint32_t bytes = mask ? mask_bytes(mask, 0, x.end, lane) : 0u;
+            uint32_t bytes = mask ? mask_bytes(mask, x.j0 * 128, x.end, lane) : 0u;
             for (int j = 0; j < x.blocks; ++j) {
-                const bool cut = mask || (j + 1) * 128 > x.end;       // some keys may be hidden
+                const int key0 = (x.j0 + j) * 128;
+                const bool cut = mask || key0 + 128 > x.end;          // some keys may be hidden
                 Seen seen;
                 if (cut) {
-                    seen = seen_of(mask, bytes, j * 128, x.end);
-                    if (mask) bytes = mask_bytes(mask, (j + 1) * 128, x.end, lane);
+                    seen = seen_of(mask, bytes, key0, x.end);
+                    if (mask) bytes = mask_bytes(mask, key0 + 128, x.end, lane);
                 }
                 wait_for(s_ready + w, n_s & 1, ok);
                 tc_fence_after_sync();
@@ -167,8 +172,9 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
                     m = top;
                 } else if (__any_sync(0xffffffffu, top - m > jump)) {
                     wait_pv();
-                    const float up = fmaxf(m, top);
-                    const float f = up == -INFINITY ? 1.f : ex2_approx((m - up) * c);
+                    // a row's reference does not depend on what its neighbours, idle lanes among them, hold
+                    const float up = top - m > jump ? top : m;
+                    const float f = up == m ? 1.f : ex2_approx((m - up) * c);
                     m = up;
                     l *= f;
 #pragma unroll
@@ -223,6 +229,26 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
                 ok = mbar_wait(pv_done + w, (n_s - 1) & 1, POLL_LIMIT) && ok;
                 tc_fence_after_sync();
             }
+            if (SPLIT) {
+                // unnormalised sums of a part, its reference maximum and denominator, for the kernel that joins them
+                float* out = a.part + ((long long)t * 2 + w) * (128 * (D + 4)) + row * (D + 4);
+#pragma unroll
+                for (int k = 0; k < D; k += 16) {
+                    uint32_t o[16];
+                    if (x.blocks) {
+                        tmem_ld_32x32b_x16(to + k, o);
+                        tmem_ld_wait();
+                    }
+#pragma unroll
+                    for (int q = 0; q < 16; q += 4)
+                        *reinterpret_cast<float4*>(out + k + q) =
+                            x.blocks ? make_float4(__uint_as_float(o[q]), __uint_as_float(o[q + 1]), __uint_as_float(o[q + 2]), __uint_as_float(o[q + 3]))
+                                     : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+                *reinterpret_cast<float2*>(out + D) = make_float2(m, l);
+                tc_fence_before_sync();
+                continue;
+            }
             const int h = x.kvh * a.group + head;
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.Oo) + ((long long)x.b * a.Nq + token) * a.o_stride + (long long)h * D;
 #pragma unroll
@@ -273,13 +299,13 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
                     mbar_expect_tx(k_full + s, S::TILE);
 #pragma unroll
                     for (int k = 0; k < S::BOXES; ++k)
-                        tma_load_4d(base + S::OFF_K + s * S::TILE + k * S::PLANE, &map_k, k_full + s, k * S::BOX, x.kvh, j * 128, x.b);
+                        tma_load_4d(base + S::OFF_K + s * S::TILE + k * S::PLANE, &map_k, k_full + s, k * S::BOX, x.kvh, (x.j0 + j) * 128, x.b);
                     if (n >= S::STAGES) ok = mbar_wait(v_empty + s, parity, POLL_LIMIT) && ok;
                     if (!ok) break;
                     mbar_expect_tx(v_full + s, S::TILE);
 #pragma unroll
                     for (int k = 0; k < S::BOXES; ++k)
-                        tma_load_4d(base + S::OFF_V + s * S::TILE + k * S::PLANE, &map_v, v_full + s, k * S::BOX, x.kvh, j * 128, x.b);
+                        tma_load_4d(base + S::OFF_V + s * S::TILE + k * S::PLANE, &map_v, v_full + s, k * S::BOX, x.kvh, (x.j0 + j) * 128, x.b);
                 }
             }
         }
@@ -365,7 +391,8 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
             const uint8_t* mask = a.key_mask ? a.key_mask + (long long)x.b * a.Nk : nullptr;
             for (int j = 0; j < x.blocks && ok; ++j, ++nv) {
                 const int sv = nv % S::STAGES;
-                const Seen seen = seen_of(mask, mask ? mask_bytes(mask, j * 128, x.end, lane) : 0u, j * 128, x.end);
+                const int key0 = (x.j0 + j) * 128;
+                const Seen seen = seen_of(mask, mask ? mask_bytes(mask, key0, x.end, lane) : 0u, key0, x.end);
                 ok = mbar_wait(v_full + sv, (nv / S::STAGES) & 1, POLL_LIMIT) && ok;
                 if ((seen.w[0] & seen.w[1] & seen.w[2] & seen.w[3]) != 0xffffffffu) {
                     constexpr int CHUNKS = S::ROW / 16;
@@ -391,44 +418,91 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
     if (warp == 9) tmem_dealloc(tmem, 512);
 }
 
+// Joins the parts of split walks: a CTA for 16 rows.
+template <int D>
+__global__ void __launch_bounds__(128) cross_attend_join_kernel(const TcArgs g) {
+    extern __shared__ float weight[];
+    const CrossArgs& a = g.a;
+    pdl_wait();
+    const int pair = blockIdx.x >> 4, w = (blockIdx.x >> 3) & 1, row0 = (blockIdx.x & 7) * 16;
+    const int p = (int)fdiv((uint32_t)pair, g.pairs_div);
+    const int b = (int)fdiv((uint32_t)p, a.kv_div), kvh = p - b * a.kv, token0 = (pair - p * g.pairs) * 2 * g.tokens + w * g.tokens;
+    const int rows = min(16, min(g.tokens, a.Nq - token0) * a.group - row0);
+    if (rows <= 0) return;
+    const long long tile = 128 * (D + 4);
+    auto place = [&](int r, int& token, int& h) {
+        const int in_token = (int)fdiv((uint32_t)(row0 + r), a.group_div);
+        token = token0 + in_token;
+        h = kvh * a.group + row0 + r - in_token * a.group;
+    };
+    cross_join<D>(a.part + ((long long)pair * g.splits * 2 + w) * tile + row0 * (D + 4), 2 * tile, D + 4, rows, g.splits, a.scale_log2, weight,
+                  [&](int r, int ch, float4 v) {
+                      int token, h;
+                      place(r, token, h);
+                      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.Oo) + ((long long)b * a.Nq + token) * a.o_stride + (long long)h * D + 4 * ch;
+                      *reinterpret_cast<uint2*>(out) = make_uint2(pack2_bf16(v.x, v.y), pack2_bf16(v.z, v.w));
+                  },
+                  [&](int r, float ref, float sum) {
+                      int token, h;
+                      place(r, token, h);
+                      if (a.lse) a.lse[((long long)b * a.heads + h) * a.Nq + token] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+                  });
+}
+
+int tile_pairs(const CrossDims& d) { return (d.Nq + 2 * (128 / d.group) - 1) / (2 * (128 / d.group)); }
+TcSplit attend_split(const CrossDims& d) { return tc_split((long long)tile_pairs(d) * d.B * d.kv, (d.Nk + 127) / 128); }
+
 template <int D>
 cudaError_t launch(const CrossDims& d, const CrossArgs& a, cudaStream_t st) {
     using S = Shape<D>;
     TcArgs g;
     g.a = a;
     g.tokens = 128 / d.group;
-    g.pairs = (d.Nq + 2 * g.tokens - 1) / (2 * g.tokens);
-    g.total = g.pairs * d.B * d.kv;
+    const TcSplit sp = attend_split(d);
+    g.pairs = tile_pairs(d);
+    g.splits = sp.splits;
+    g.part = sp.part;
+    g.total = g.pairs * d.B * d.kv * g.splits;
     g.pairs_div = fast_div(g.pairs);
+    g.splits_div = fast_div(g.splits);
     CUtensorMap q, k, v;
     if (!rows_map(&q, a.Q, D, d.heads, d.Nq, d.B, d.q_stride, S::BOX, d.group, g.tokens) ||
         !rows_map(&k, a.K, D, d.kv, d.Nk, d.B, d.k_stride, S::BOX, 1, 128) || !rows_map(&v, a.V, D, d.kv, d.Nk, d.B, d.v_stride, S::BOX, 1, 128))
         return cudaErrorInvalidValue;
     static PerDeviceOnce attr;
     const cudaError_t e = attr.run([&] {
-        return cudaFuncSetAttribute(cross_attend_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::smem);
+        const cudaError_t f = cudaFuncSetAttribute(cross_attend_tc_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::smem);
+        return f != cudaSuccess ? f : cudaFuncSetAttribute(cross_attend_tc_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::smem);
     });
     if (e != cudaSuccess) return e;
-    cross_attend_tc_kernel<D><<<g.total < kSMs ? g.total : kSMs, THREADS, S::smem, st>>>(g, q, k, v);
+    const int ctas = g.total < kSMs ? g.total : kSMs;
+    if (g.splits > 1) cross_attend_tc_kernel<D, true><<<ctas, THREADS, S::smem, st>>>(g, q, k, v);
+    else              cross_attend_tc_kernel<D, false><<<ctas, THREADS, S::smem, st>>>(g, q, k, v);
     count_launch();
-    return cudaGetLastError();
+    cudaError_t f = cudaGetLastError();
+    if (f != cudaSuccess || g.splits == 1) return f;
+    f = launch_kernel(cross_attend_join_kernel<D>, dim3(g.pairs * d.B * d.kv * 16), dim3(128), sizeof(float) * 16 * (g.splits + 1), st, true, g);
+    if (f == cudaSuccess) count_launch();
+    return f;
 }
 
 }  // namespace
 
-// Measured (B200, us, this kernel / the warp-level one).  One block of keys: 8 pairs of tiles of 8 heads of 32 6.4 / 3.4, 64 pairs
-// 6.1 / 4.8, 128 pairs 6.2 / 6.6, 512 pairs 16.7 / 18.2 (64 x 196 x 100).  Two blocks: 8 to 128 pairs 7.7 - 8.0 / 6.5 - 9.6; more:
-// 16 x 1024 x 1024, 12 heads of 64 97 / 195, 2 x 4133 x 4096, 37 heads of 32 474 / 744, of 64 480 / 1138, of 128 643 / 2056.
-// Few pairs and many blocks, where the other one splits the keys: 1 x 196 x 1024, 8 heads of 32 17.4 / 10.5, 2 images 17.5 / 16.0,
-// 4 images 17.5 / 15.9, 16 images 18.1 / 27.1; 1 x 100 x 2048, 8 heads of 64 22.8 / 19.0; at head dim 128 it pays all the same (1 x 1024 x
-// 2048, 4 heads 39.6 / 56.2).
+size_t cross_attend_tc_part(const CrossDims& d) {
+    const TcSplit s = attend_split(d);
+    return s.splits > 1 ? (size_t)tile_pairs(d) * d.B * d.kv * s.splits * 2 * 128 * (d.D + 4) : 0;
+}
+
+// Measured (B200, us, this kernel / the warp-level one).  One block of keys: 64 x 4096 x 20, 4 heads of 32 100 / 96; up to 64 pairs of tiles
+// (8 x 196 x 128, 8 heads of 32) 6.1 / 4.8; 128 pairs 6.2 / 6.6; 4 x 1024 x 100, 8 heads of 64 8.2 / 10.2.  More blocks: 8 x 196 x 256 7.8 / 6.5,
+// 16 x 196 x 256 8.7 / 9.6, 1 x 100 x 512, 8 heads of 64 9.0 / 16.3, 4 x 100 x 2048 16.3 / 31.5, 1 x 1024 x 2048, 4 heads of 128 24 / 57,
+// 2 x 4133 x 4096, 37 heads of 32 474 / 744, of 64 480 / 1137, of 128 643 / 2055.  At most 64 rows: half of a tile and more is empty, and the
+// warp-level kernel splits the keys over more CTAs (16 rows and less have a form of their own there).
 bool cross_attend_tc_pays(const CrossDims& d) {
-    if (d.D < 32 || d.group > 128 || d.rows <= 64) return false;
-    const int tokens = 128 / d.group;
-    const long long pairs = ((long long)d.Nq + 2 * tokens - 1) / (2 * tokens) * d.B * d.kv;
-    if (pairs > (1 << 30)) return false;
-    if (d.Nk <= 128) return pairs >= 128;
-    return d.Nk <= 896 || pairs > 16 || d.D == 128;
+    if (d.D < 32 || d.group > 128 || d.esize != 2) return false;
+    const long long pairs = (long long)tile_pairs(d) * d.B * d.kv;
+    if (pairs > (1 << 26)) return false;
+    return d.rows > 64 && (d.Nk > 128 || (d.Nk > 64 && pairs >= 128));
 }
 
 cudaError_t launch_cross_attend_tc(const CrossDims& d, CrossArgs a, cudaStream_t st) {

@@ -47,11 +47,13 @@ struct TcArgs {
     int tokens;             // of a tile of rows: 128 / group
     int row_blocks;         // of a pair
     int tiles;              // kept tiles of a pair
-    int total;
-    FastDiv tiles_div;
+    int splits, part;       // parts of a walk and their length in blocks
+    int total;              // parts of all tiles of all pairs
+    FastDiv tiles_div, splits_div;
 };
 
-template <int D, bool DKV>
+// SPLIT: walks are cut in parts
+template <int D, bool DKV, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
 cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_do) {
@@ -87,15 +89,19 @@ cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, 
     pdl_launch_dependents();
 
     // every role walks the same tiles
-    struct Tile { int p, b, kvh, x0, end, blocks; };         // x0: first token of the kept tile (a query's or a key)
+    // x0: first token of the kept tile (a query's or a key); j0: first block of this part of its walk
+    struct Tile { int p, b, kvh, x0, end, j0, blocks; };
     auto tile_of = [&](int t) {
         Tile x;
-        x.p = (int)fdiv((uint32_t)t, g.tiles_div);
-        x.x0 = (t - x.p * g.tiles) * (DKV ? 128 : g.tokens);
+        const int tile = SPLIT ? (int)fdiv((uint32_t)t, g.splits_div) : t;
+        x.j0 = SPLIT ? (t - tile * g.splits) * g.part : 0;
+        x.p = (int)fdiv((uint32_t)tile, g.tiles_div);
+        x.x0 = (tile - x.p * g.tiles) * (DKV ? 128 : g.tokens);
         x.b = (int)fdiv((uint32_t)x.p, a.kv_div);
         x.kvh = x.p - x.b * a.kv;
         x.end = cross_key_end(a, x.b);
         x.blocks = DKV ? (x.x0 < x.end ? g.row_blocks : 0) : (x.end + 127) >> 7;
+        if (SPLIT) x.blocks = min(max(x.blocks - x.j0, 0), g.part);
         return x;
     };
 
@@ -119,17 +125,18 @@ cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, 
                 nd = __ldcg(st + 128);
             }
             const float2 nl2 = make_float2(nl, nl), nd2 = make_float2(nd, nd);
-            uint32_t bytes = !DKV && mask ? mask_bytes(mask, 0, x.end, lane) : 0u;
+            uint32_t bytes = !DKV && mask ? mask_bytes(mask, x.j0 * 128, x.end, lane) : 0u;
             for (int j = 0; j < x.blocks; ++j, ++n) {
                 const int stage = n % S::STAGES;
                 const uint32_t stat = base + S::OFF_STAT + stage * 1024 + half * 256;
-                const bool cut = !DKV && (mask || (j + 1) * 128 > x.end);        // some keys may be hidden
+                const int key0 = (x.j0 + j) * 128;
+                const bool cut = !DKV && (mask || key0 + 128 > x.end);            // some keys may be hidden
                 uint32_t see[2] = {0u, 0u};
                 if (cut) {
-                    const Seen seen = seen_of(mask, bytes, j * 128, x.end);
+                    const Seen seen = seen_of(mask, bytes, key0, x.end);
                     see[0] = seen.w[2 * half];
                     see[1] = seen.w[2 * half + 1];
-                    if (mask) bytes = mask_bytes(mask, (j + 1) * 128, x.end, lane);
+                    if (mask) bytes = mask_bytes(mask, key0 + 128, x.end, lane);
                 }
                 if (DKV) wait_for(y_full + stage, (n / S::STAGES) & 1, ok);       // the rows' statistics
                 wait_for(s_ready, n & 1, ok);
@@ -224,7 +231,26 @@ cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, 
                 if (DKV) wait_for(pv_done, (n - 1) & 1, ok);
                 tc_fence_after_sync();
             }
-            if (DKV) {
+            if (SPLIT) {
+                // fp32 sums of a part, for the kernel that adds them; one warpgroup dK, the other dV, or half of dQ's channels each
+                constexpr int COLS = DKV ? D : D / 2;
+                bool live = ok;
+                if (DKV && live) live = x.x0 + row < x.end && (!mask || __ldg(mask + x.x0 + row) != 0);
+                float* out = a.part + ((long long)t * (DKV ? 2 : 1) + (DKV ? half : 0)) * (128 * D) + row * D + (DKV ? 0 : half * COLS);
+#pragma unroll
+                for (int k = 0; k < COLS; k += 16) {
+                    uint32_t o[16];
+                    if (x.blocks) {
+                        tmem_ld_32x32b_x16(tl + (DKV && half ? S::TM_A2 : S::TM_A1) + (DKV ? 0 : half * COLS) + k, o);
+                        tmem_ld_wait();
+                    }
+#pragma unroll
+                    for (int q = 0; q < 16; q += 4)
+                        *reinterpret_cast<float4*>(out + k + q) =
+                            live && x.blocks ? make_float4(__uint_as_float(o[q]), __uint_as_float(o[q + 1]), __uint_as_float(o[q + 2]), __uint_as_float(o[q + 3]))
+                                             : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+            } else if (DKV) {
                 // one warpgroup stores dK, the other dV; thread = key
                 const int key = x.x0 + row;
                 bool live = key < x.end;
@@ -304,14 +330,14 @@ cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, 
                     if (n >= S::STAGES) ok = mbar_wait(y_empty + s, (n / S::STAGES - 1) & 1, POLL_LIMIT) && ok;
                     if (!ok) break;
                     mbar_expect_tx(y_full + s, 2 * S::BOXES * (DKV ? rows_box : keys_box) + (DKV ? 1024 : 0));
-                    const int y0 = j * (DKV ? g.tokens : 128);
+                    const int y0 = (x.j0 + j) * (DKV ? g.tokens : 128);
 #pragma unroll
                     for (int k = 0; k < S::BOXES; ++k) {
                         const uint32_t to = base + S::OFF_Y + s * S::STAGE + k * S::PLANE;
                         tma_load_4d(to, DKV ? &map_q : &map_k, y_full + s, k * S::BOX, DKV ? x.kvh * a.group : x.kvh, y0, x.b);
                         tma_load_4d(to + S::TILE, DKV ? &map_do : &map_v, y_full + s, k * S::BOX, DKV ? x.kvh * a.group : x.kvh, y0, x.b);
                     }
-                    if (DKV) bulk_load(base + S::OFF_STAT + s * 1024, g.stats + ((long long)x.p * g.row_blocks + j) * 256, 1024, y_full + s);
+                    if (DKV) bulk_load(base + S::OFF_STAT + s * 1024, g.stats + ((long long)x.p * g.row_blocks + x.j0 + j) * 256, 1024, y_full + s);
                 }
             }
         }
@@ -386,7 +412,8 @@ cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, 
             const uint8_t* mask = a.key_mask ? a.key_mask + (long long)x.b * a.Nk : nullptr;
             for (int j = 0; j < x.blocks && ok; ++j, ++n) {
                 const int s = n % S::STAGES;
-                const Seen seen = seen_of(mask, mask ? mask_bytes(mask, j * 128, x.end, lane) : 0u, j * 128, x.end);
+                const int key0 = (x.j0 + j) * 128;
+                const Seen seen = seen_of(mask, mask ? mask_bytes(mask, key0, x.end, lane) : 0u, key0, x.end);
                 ok = mbar_wait(y_full + s, (n / S::STAGES) & 1, POLL_LIMIT) && ok;
                 if ((seen.w[0] & seen.w[1] & seen.w[2] & seen.w[3]) != 0xffffffffu) {
                     constexpr int CHUNKS = S::ROW / 16;
@@ -450,7 +477,74 @@ __global__ void __launch_bounds__(256) cross_stats_kernel(const TcArgs g, float*
     }
 }
 
+// Adds the parts of split walks in order: thread = four channels of a kept row.
+template <int D, bool DKV>
+__global__ void __launch_bounds__(256) cross_grad_join_kernel(const TcArgs g, int pairs) {
+    const CrossArgs& a = g.a;
+    pdl_wait();
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int ch = (int)(i % (D / 4)) * 4, row = (int)(i / (D / 4)) & 127;
+    const long long rest = i / (D / 4) / 128;
+    const int which = DKV ? (int)(rest & 1) : 0;
+    const long long tile = DKV ? rest >> 1 : rest;
+    if (tile >= (long long)pairs * g.tiles) return;
+    const int p = (int)(tile / g.tiles), x0 = (int)(tile - (long long)p * g.tiles) * (DKV ? 128 : g.tokens);
+    const int b = (int)fdiv((uint32_t)p, a.kv_div), kvh = p - b * a.kv;
+    __nv_bfloat16* out;
+    if (DKV) {
+        if (x0 + row >= a.Nk) return;
+        const long long key = (long long)b * a.Nk + x0 + row;
+        out = (which ? static_cast<__nv_bfloat16*>(a.dV) + key * a.v_stride : static_cast<__nv_bfloat16*>(a.dK) + key * a.k_stride) + (long long)kvh * D;
+    } else {
+        const int in_token = (int)fdiv((uint32_t)row, a.group_div), token = x0 + in_token;
+        if (in_token >= g.tokens || token >= a.Nq) return;
+        out = static_cast<__nv_bfloat16*>(a.dQ) + ((long long)b * a.Nq + token) * a.q_stride + (long long)(kvh * a.group + row - in_token * a.group) * D;
+    }
+    const float* from = a.part + (tile * g.splits * (DKV ? 2 : 1) + which) * (128 * D) + row * D + ch;
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int s = 0; s < g.splits; ++s) {
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(from + (long long)s * (DKV ? 2 : 1) * (128 * D)));
+        t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+    }
+    const float f = which ? 1.f : a.scale;
+    *reinterpret_cast<uint2*>(out + ch) = make_uint2(pack2_bf16(t.x * f, t.y * f), pack2_bf16(t.z * f, t.w * f));
+}
+
 int row_blocks(const CrossDims& d) { return (d.Nq + 128 / d.group - 1) / (128 / d.group); }
+
+// Fewer kept tiles than SMs: walks are split, one part for an SM at most.
+TcSplit grad_split(const CrossDims& d, bool dkv) {
+    return tc_split((long long)d.B * d.kv * (dkv ? (d.Nk + 127) / 128 : row_blocks(d)), dkv ? row_blocks(d) : (d.Nk + 127) / 128);
+}
+
+template <int D, bool DKV>
+cudaError_t launch_grad(const CrossDims& d, TcArgs g, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, const CUtensorMap& o, cudaStream_t st) {
+    const TcSplit sp = grad_split(d, DKV);
+    const int pairs = d.B * d.kv;
+    g.tiles = DKV ? (d.Nk + 127) / 128 : g.row_blocks;
+    g.splits = sp.splits;
+    g.part = sp.part;
+    g.total = pairs * g.tiles * g.splits;
+    g.tiles_div = fast_div(g.tiles);
+    g.splits_div = fast_div(g.splits);
+    static PerDeviceOnce attr;
+    cudaError_t e = attr.run([&] {
+        const cudaError_t f = cudaFuncSetAttribute(cross_grad_tc_kernel<D, DKV, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<D, DKV>::smem);
+        return f != cudaSuccess ? f : cudaFuncSetAttribute(cross_grad_tc_kernel<D, DKV, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<D, DKV>::smem);
+    });
+    if (e != cudaSuccess) return e;
+    const dim3 ctas(g.total < kSMs ? g.total : kSMs), threads_of(THREADS);
+    e = g.splits > 1 ? launch_kernel(cross_grad_tc_kernel<D, DKV, true>, ctas, threads_of, Shape<D, DKV>::smem, st, true, g, q, k, v, o)
+                     : launch_kernel(cross_grad_tc_kernel<D, DKV, false>, ctas, threads_of, Shape<D, DKV>::smem, st, true, g, q, k, v, o);
+    if (e != cudaSuccess) return e;
+    count_launch();
+    if (g.splits == 1) return cudaSuccess;
+    const long long threads = (long long)pairs * g.tiles * (DKV ? 2 : 1) * 128 * (D / 4);
+    e = launch_kernel(cross_grad_join_kernel<D, DKV>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, true, g, pairs);
+    if (e == cudaSuccess) count_launch();
+    return e;
+}
 
 template <int D>
 cudaError_t launch(const CrossDims& d, const CrossArgs& a, cudaStream_t st) {
@@ -466,44 +560,35 @@ cudaError_t launch(const CrossDims& d, const CrossArgs& a, cudaStream_t st) {
     if (!rows_map(&q, a.Q, D, d.heads, d.Nq, d.B, d.q_stride, BOX, d.group, g.tokens) || !rows_map(&k, a.K, D, d.kv, d.Nk, d.B, d.k_stride, BOX, 1, 128) ||
         !rows_map(&v, a.V, D, d.kv, d.Nk, d.B, d.v_stride, BOX, 1, 128) || !rows_map(&o, a.dO, D, d.heads, d.Nq, d.B, d.o_stride, BOX, d.group, g.tokens))
         return cudaErrorInvalidValue;
-    static PerDeviceOnce attr;
-    cudaError_t e = attr.run([&] {
-        const cudaError_t f = cudaFuncSetAttribute(cross_grad_tc_kernel<D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<D, false>::smem);
-        return f != cudaSuccess ? f : cudaFuncSetAttribute(cross_grad_tc_kernel<D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Shape<D, true>::smem);
-    });
-    if (e != cudaSuccess) return e;
-    g.tiles = 1;
+    cudaError_t e;
     g.total = pairs;
     const long long lanes = (long long)pairs * g.row_blocks * 128 * (D / 8);
     cross_stats_kernel<D><<<(unsigned)((lanes + 255) / 256), 256, 0, st>>>(g, stats);
     count_launch();
     if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    g.tiles = g.row_blocks;
-    g.total = pairs * g.tiles;
-    g.tiles_div = fast_div(g.tiles);
-    e = launch_kernel(cross_grad_tc_kernel<D, false>, dim3(g.total < kSMs ? g.total : kSMs), dim3(THREADS), Shape<D, false>::smem, st, true, g, q, k, v, o);
-    if (e != cudaSuccess) return e;
-    count_launch();
-    g.tiles = (d.Nk + 127) / 128;
-    g.total = pairs * g.tiles;
-    g.tiles_div = fast_div(g.tiles);
-    e = launch_kernel(cross_grad_tc_kernel<D, true>, dim3(g.total < kSMs ? g.total : kSMs), dim3(THREADS), Shape<D, true>::smem, st, true, g, q, k, v, o);
-    if (e != cudaSuccess) return e;
-    count_launch();
-    return cudaSuccess;
+    if ((e = launch_grad<D, false>(d, g, q, k, v, o, st)) != cudaSuccess) return e;
+    return launch_grad<D, true>(d, g, q, k, v, o, st);
 }
 
 }  // namespace
 
 size_t cross_backward_tc_stats(const CrossDims& d) { return sizeof(float) * 256 * (size_t)d.B * d.kv * row_blocks(d); }
 
+size_t cross_backward_tc_part(const CrossDims& d) {
+    const TcSplit q = grad_split(d, false), k = grad_split(d, true);
+    const size_t pairs = (size_t)d.B * d.kv, tile = 128 * (size_t)d.D;
+    const size_t nq = q.splits > 1 ? pairs * row_blocks(d) * q.splits * tile : 0, nk = k.splits > 1 ? pairs * ((d.Nk + 127) / 128) * k.splits * 2 * tile : 0;
+    return nq > nk ? nq : nk;
+}
+
+// Measured (B200, us, these kernels / the warp-level ones): 1 x 196 x 100, 8 heads of 32 12.7 / 13.2, 64 images 40 / 43; 16 x 100 x 100, 8 heads
+// of 64 13 / 16; 4 x 64 x 512 14.4 / 19.5; 1 x 4096 x 77, 4 heads of 32 17 / 30; 4 x 1024 x 512, 4 heads of 128 36 / 88; 16 x 1024 x 1024, 12 heads of
+// 64 262 / 621.  At most 64 rows: half of a tile and more is empty.
 bool cross_backward_tc_pays(const CrossDims& d) {
     if (d.D < 32 || d.group > 128 || d.esize != 2) return false;
     const long long pairs = (long long)d.B * d.kv;
-    if (pairs * row_blocks(d) > (1 << 24) || pairs * ((d.Nk + 127) / 128) > (1 << 30)) return false;
-    static const char* force = getenv("BRA_TC");
-    if (force) return force[0] == '1';
-    return d.rows >= 128 && d.Nk >= 128;
+    if (pairs * row_blocks(d) > (1 << 24) || pairs * ((d.Nk + 127) / 128) > (1 << 24)) return false;
+    return d.rows > 64;
 }
 
 cudaError_t launch_cross_backward_tc(const CrossDims& d, CrossArgs a, cudaStream_t st) {

@@ -61,6 +61,8 @@ cudaError_t launch_cross_attend_tc(const CrossDims& d, CrossArgs a, cudaStream_t
 cudaError_t launch_cross_backward_mma(const CrossDims& d, CrossArgs a, cudaStream_t st);
 bool cross_backward_tc_pays(const CrossDims& d);
 size_t cross_backward_tc_stats(const CrossDims& d);         // bytes of its rows' statistics
+size_t cross_backward_tc_part(const CrossDims& d);
+size_t cross_attend_tc_part(const CrossDims& d);
 cudaError_t launch_cross_backward_tc(const CrossDims& d, CrossArgs a, cudaStream_t st);
 cudaError_t launch_cross_attend_simt(const CrossDims& d, CrossArgs a, cudaStream_t st);
 cudaError_t launch_cross_backward_simt(const CrossDims& d, CrossArgs a, cudaStream_t st);

@@ -36,6 +36,21 @@ __device__ __forceinline__ void wait_for(uint64_t* bar, uint32_t parity, bool& o
     if (!mbar_try_wait(bar, parity)) ok = mbar_wait(bar, parity, POLL_LIMIT) && ok;
 }
 
+// Work for fewer CTAs than SMs: every walk of `blocks` blocks is cut in parts, as many as make one part an SM at most.  Joining the parts
+// costs about what three blocks do (8 pairs of tiles, 8 heads of 32, forward, whole / cut, us: 2 blocks 7.7 / 9.5, 4 blocks 11.0 / 10.4,
+// 8 blocks 17.4 / 11.1).
+struct TcSplit { int splits, part; };
+inline TcSplit tc_split(long long tiles, int blocks) {
+    long long splits = tiles > 0 ? kSMs / tiles : 1;
+    if (splits > blocks) splits = blocks;
+    if (splits < 1) splits = 1;
+    TcSplit s;
+    s.part = (int)((blocks + splits - 1) / splits);
+    if (blocks - s.part < 3) s.part = blocks;
+    s.splits = (blocks + s.part - 1) / s.part;
+    return s;
+}
+
 // [B, tokens, heads, D] with `stride` elements from token to token; box: BOX channels x heads x tokens of one image
 inline bool rows_map(CUtensorMap* m, const void* base, int D, int heads, long long tokens, int B, long long stride, int box_ch, int box_heads, int box_tokens) {
     EncodeTiledFn enc = tma_encoder();

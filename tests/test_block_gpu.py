@@ -235,6 +235,24 @@ CROSS = [
 ]
 
 
+# Where the tcgen05 kernels run: more than 64 rows a key head, more than a block of keys (or many tiles)
+CROSS_WIDE = [
+    (2, 300, 400, 4, 4, 32, [400, 129], True),
+    (2, 257, 640, 6, 2, 64, [0, 640], False),                # a group of three: 126 of a tile's 128 rows
+    (1, 700, 700, 5, 1, 128, None, True),                    # a group of five
+    (20, 100, 130, 8, 8, 64, None, False),                   # more tiles than SMs, one of a pair
+    (24, 140, 90, 8, 8, 32, [(11 * i) % 91 for i in range(24)], False),     # one block of keys
+    (19, 300, 300, 8, 8, 32, [300 - 16 * i for i in range(19)], True),      # CTAs with several pairs of different lengths
+    (11, 260, 257, 8, 8, 128, None, False),
+    (1, 3000, 200, 1, 1, 64, [150], False),                  # walks over the queries are split
+    (1, 130, 3000, 1, 1, 128, [2900], True),                 # walks over the keys are split
+    (1, 300, 1300, 2, 2, 32, [257], False),                  # and most parts have nothing to do
+    (1, 3, 300, 100, 1, 32, None, False),                    # a group of a hundred: a token a tile
+    (1, 2, 300, 128, 1, 64, None, True),
+    (1, 2, 300, 130, 1, 32, None, False),                    # a group larger than a tile
+]
+
+
 def cross_problem(bra, case, dtype, seed=0, **kw):
     import torch
     B, Nq, Nk, heads, kv, D, lens, masked = case
@@ -274,6 +292,26 @@ def test_cross(bra, case, dtype):
     check_cross(bra, *cross_problem(bra, case, dtype), dtype)
 
 
+@pytest.mark.parametrize("case", CROSS_WIDE, ids=str)
+def test_cross_wide(bra, case):
+    check_cross(bra, *cross_problem(bra, case, "bf16"), "bf16")
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_cross_wide_many_launches(bra, D):
+    """Long walks of many tiles, again and again, forward and backward: the same bits, no wait that gives up."""
+    import torch
+    p, Q, K, V, dO, _, _, _ = cross_problem(bra, (4, 1000, 1100, 20, 10, D, None, False), "bf16")
+    ws = bra.cross_workspace(p)
+    first = None
+    for _ in range(10):
+        O, lse = bra.bra_cross_attend(p, Q, K, V, ws=ws)
+        got = (O, lse) + bra.bra_cross_backward(p, Q, K, V, O, lse, dO, ws=ws)
+        first = got if first is None else first
+        assert all(torch.equal(a, b) for a, b in zip(first, got))
+    assert bra.bra_device_status(ws) == 0
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("D", [16, 32, 64, 128])
 @pytest.mark.parametrize("Nq,Nk", [(1, 2), (16, 17), (17, 31), (63, 33), (64, 65), (66, 128), (128, 129), (255, 257)])
@@ -304,7 +342,9 @@ def test_cross_on_slices_and_with_a_scale(bra, dtype):
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("case", [(2, 1, 300, 4, 2, 64, [300, 170], True), (2, 80, 200, 4, 2, 32, [200, 0], True),
-                                  (2, 200, 70, 2, 2, 128, [33, 70], True), (1, 300, 400, 2, 2, 64, [257], False)], ids=str)
+                                  (2, 200, 70, 2, 2, 128, [33, 70], True), (1, 300, 400, 2, 2, 64, [257], False),
+                                  (3, 200, 300, 6, 2, 32, [300, 0, 130], True), (2, 300, 520, 2, 2, 128, [520, 300], True),
+                                  (1, 2000, 140, 2, 1, 64, [129], True)], ids=str)
 def test_cross_hidden_keys_reach_nothing(bra, case, dtype, bad):
     """Outputs and gradients to the same bits, whatever stands in hidden keys and values."""
     import torch
@@ -343,7 +383,7 @@ def test_cross_large_scores(bra, dtype):
 
 def test_cross_is_the_same_every_time_and_on_other_streams(bra):
     import torch
-    for case in (CROSS[2], CROSS[11], CROSS[13]):
+    for case in (CROSS[2], CROSS[11], CROSS[13], CROSS_WIDE[1], CROSS_WIDE[7], CROSS_WIDE[8]):
         p, Q, K, V, dO, key_len, key_mask, _ = cross_problem(bra, case, "bf16")
         ws = bra.cross_workspace(p)
         O, lse = bra.bra_cross_attend(p, Q, K, V, key_len, key_mask, ws=ws)
