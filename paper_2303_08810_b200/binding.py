@@ -321,14 +321,26 @@ def bra_device_status(ws, stream=None) -> int:
 # These calls take tensors of a program's own making (slices of fused projections, masks, positions), so what a wrong one would
 # make the kernels read is checked here: element type, number of elements, order in memory, device.
 _DTYPES = {"f32": F32, "bf16": BF16, F32: F32, BF16: BF16}
+_GET_DEVICE = None
 
 
-def _tensor(t, name, where, dtype, numel, device, optional=False, tokens=None):
-    """Address of a dense tensor of `numel` elements on the current device; with tokens = (images, tokens, channels, stride) of a
-    [images, tokens, channels] view whose tokens lie `stride` elements apart."""
+def _current_device():
+    global _GET_DEVICE
+    if _GET_DEVICE is None:
+        torch = _torch()
+        _GET_DEVICE = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _GET_DEVICE()
+
+
+def _at(t, name, where, dtype, numel, device):
+    """Address of a dense tensor of `numel` elements on the current device."""
+    if t is not None and t.dtype is dtype and t.numel() == numel and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
+    return _refuse(t, name, where, dtype, numel, device)
+
+
+def _refuse(t, name, where, dtype, numel, device):
     if t is None:
-        if optional:
-            return None
         raise BraError(1, f"{where}: {name}")
     if t.dtype is not dtype:
         raise BraError(4, f"{where}: {name} is {t.dtype}, not {dtype}")
@@ -336,28 +348,41 @@ def _tensor(t, name, where, dtype, numel, device, optional=False, tokens=None):
         raise ValueError(f"{where}: {name} is on {t.device}, the current device is cuda:{device}")
     if t.numel() != numel:
         raise BraError(2, f"{where}: {name} has {t.numel()} elements, not {numel}")
-    if tokens is not None:
-        B, N, C, stride = tokens
-        if stride != C:
-            if t.dim() != 3 or tuple(t.shape) != (B, N, C) or (C > 1 and t.stride(2) != 1) or (N > 1 and t.stride(1) != stride) or \
-                    (B > 1 and t.stride(0) != N * stride):
-                raise BraError(2, f"{where}: {name} is not a [{B}, {N}, {C}] view with {stride} elements from token to token")
-            return t.data_ptr()
-    if not t.is_contiguous():
-        raise BraError(2, f"{where}: {name} is not contiguous")
+    raise BraError(2, f"{where}: {name} is not contiguous")
+
+
+def _rows_at(t, name, where, dtype, device, tokens):
+    """Address of a tensor of tokens = (images, tokens, channels, stride, elements): dense, or a [images, tokens, channels] view whose
+    tokens lie `stride` elements apart."""
+    B, N, C, stride, numel = tokens
+    if stride == C:
+        return _at(t, name, where, dtype, numel, device)
+    if t is None or t.dtype is not dtype or t.get_device() != device or t.numel() != numel:
+        return _refuse(t, name, where, dtype, numel, device)
+    if t.dim() != 3 or tuple(t.shape) != (B, N, C) or (C > 1 and t.stride(2) != 1) or (N > 1 and t.stride(1) != stride) or \
+            (B > 1 and t.stride(0) != N * stride):
+        raise BraError(2, f"{where}: {name} is not a [{B}, {N}, {C}] view with {stride} elements from token to token")
     return t.data_ptr()
 
 
-def _current_device():
-    torch = _torch()
-    get = getattr(torch._C, "_cuda_getDevice", None)
-    return get() if get else torch.cuda.current_device()
+# What a call derives from its problem, by the problem's bytes: small calls are bound by their marshalling.
+_DERIVED = {}
+
+
+def _derived(p, make):
+    key = bytes(p)
+    d = _DERIVED.get((make, key))
+    if d is None:
+        if len(_DERIVED) > 4096:
+            _DERIVED.clear()
+        d = _DERIVED[make, key] = make(p)
+    return d
 
 
 def _like(t, tokens):
     """A new tensor laid out as `t` (a slice of channels of a wider tensor stays one)."""
     torch = _torch()
-    B, N, C, stride = tokens
+    B, N, C, stride, _ = tokens
     if stride == C:
         return torch.empty_like(t)
     return torch.empty(B, N, stride, dtype=t.dtype, device=t.device)[..., :C]
@@ -387,22 +412,35 @@ def rope_frequencies(rot_dim, axes=1, base=10000.0, scaling="none", factor=1.0, 
     return out.to(device)
 
 
+def _rope_derived(p):
+    q, k, n = p.heads * p.head_dim, p.kv_heads * p.head_dim, p.B * p.N
+    return (_tdtype(p), (p.B, p.N, q, p.q_stride or q, n * q), (p.B, p.N, k, p.k_stride or k, n * k),
+            p.rot_dim // p.axes // 2 if p.axes else 0, n * p.axes)
+
+
 def bra_rope(p, Q, K, freq, positions=None, Qo=None, Ko=None, inverse=False, stream=None):
     """bra_rope: Q, K -> (Qo, Ko).  Pass Q and K as Qo and Ko to rotate in place; inverse=True is the gradient's rotation."""
-    torch = _torch()
-    dev, t, where = _current_device(), _tdtype(p), "bra_rope"
-    q = (p.B, p.N, p.heads * p.head_dim, p.q_stride or p.heads * p.head_dim)
-    k = (p.B, p.N, p.kv_heads * p.head_dim, p.k_stride or p.kv_heads * p.head_dim)
-    n = p.B * p.N
-    q_at = _tensor(Q, "Q", where, t, n * q[2], dev, tokens=q)
-    k_at = _tensor(K, "K", where, t, n * k[2], dev, optional=not p.kv_heads, tokens=k)
-    f_at = _tensor(freq, "freq", where, torch.float64, p.rot_dim // p.axes // 2 if p.axes else 0, dev)
-    at = _tensor(positions, "positions", where, torch.int32, n * p.axes, dev, optional=True)
-    Qo = _like(Q, q) if Qo is None else Qo
-    Ko = _like(K, k) if Ko is None and K is not None else Ko
-    _check(load_library().bra_rope(ctypes.byref(p), q_at, k_at, at, f_at, int(bool(inverse)),
-                                   _tensor(Qo, "Qo", where, t, n * q[2], dev, tokens=q),
-                                   _tensor(Ko, "Ko", where, t, n * k[2], dev, optional=not p.kv_heads, tokens=k), _stream(stream)), where)
+    torch, dev, where = _torch(), _current_device(), "bra_rope"
+    t, q, k, pairs, places = _derived(p, _rope_derived)
+    q_at = _rows_at(Q, "Q", where, t, dev, q)
+    k_at = _rows_at(K, "K", where, t, dev, k) if k[2] or K is not None else None
+    f_at = _at(freq, "freq", where, torch.float64, pairs, dev)
+    at = None if positions is None else _at(positions, "positions", where, torch.int32, places, dev)
+    if Qo is None:
+        Qo = _like(Q, q)
+        qo_at = Qo.data_ptr()
+    else:
+        qo_at = _rows_at(Qo, "Qo", where, t, dev, q)
+    if k_at is None:
+        ko_at = None
+    elif Ko is None:
+        Ko = _like(K, k)
+        ko_at = Ko.data_ptr()
+    else:
+        ko_at = _rows_at(Ko, "Ko", where, t, dev, k)
+    code = (_LIB or load_library()).bra_rope(ctypes.byref(p), q_at, k_at, at, f_at, 1 if inverse else 0, qo_at, ko_at, _stream(stream))
+    if code:
+        raise BraError(code, where)
     return Qo, Ko
 
 
@@ -421,55 +459,61 @@ def cross_workspace(p: BraCrossProblem, device="cuda"):
     return _scratch(cross_workspace_bytes(p), "bra_cross_workspace_bytes", device)
 
 
-def _cross_tokens(p):
+def _cross_derived(p):
     C, Ck = p.heads * p.head_dim, p.kv_heads * p.head_dim
-    return (p.B, p.Nq, C, p.q_stride or C), (p.B, p.Nk, Ck, p.k_stride or Ck), (p.B, p.Nk, Ck, p.v_stride or Ck), (p.B, p.Nq, C, C)
+    nq, nk = p.B * p.Nq * C, p.B * p.Nk * Ck
+    return (_tdtype(p), (p.B, p.Nq, C, p.q_stride or C, nq), (p.B, p.Nk, Ck, p.k_stride or Ck, nk), (p.B, p.Nk, Ck, p.v_stride or Ck, nk),
+            nq, p.B, p.B * p.Nk, (p.B, p.heads, p.Nq), p.B * p.heads * p.Nq)
 
 
-def _cross_mask(p, key_len, key_mask, where, dev):
-    torch = _torch()
-    len_at = _tensor(key_len, "key_len", where, torch.int32, p.B, dev, optional=True)
-    if key_mask is not None and key_mask.dtype is torch.bool:
-        return len_at, _tensor(key_mask, "key_mask", where, torch.bool, p.B * p.Nk, dev)
-    return len_at, _tensor(key_mask, "key_mask", where, torch.uint8, p.B * p.Nk, dev, optional=True)
+def _cross_mask(key_len, key_mask, where, torch, B, keys, dev):
+    return (None if key_len is None else _at(key_len, "key_len", where, torch.int32, B, dev),
+            None if key_mask is None else
+            _at(key_mask, "key_mask", where, torch.bool if key_mask.dtype is torch.bool else torch.uint8, keys, dev))
 
 
 def bra_cross_attend(p, Q, K, V, key_len=None, key_mask=None, O=None, lse=None, ws=None, stream=None, want_lse=True):
     """bra_cross_attend: Q, K, V -> (O, lse).  key_len int32 [B], key_mask bool or uint8 [B, Nk]."""
-    torch = _torch()
-    dev, t, where = _current_device(), _tdtype(p), "bra_cross_attend"
-    q, k, v, o = _cross_tokens(p)
-    nq, nk = p.B * p.Nq * q[2], p.B * p.Nk * k[2]
-    ins = [_tensor(Q, "Q", where, t, nq, dev, tokens=q), _tensor(K, "K", where, t, nk, dev, tokens=k),
-           _tensor(V, "V", where, t, nk, dev, tokens=v), *_cross_mask(p, key_len, key_mask, where, dev)]
-    ws = cross_workspace(p, Q.device) if ws is None else ws
-    O = torch.empty(Q.shape, dtype=Q.dtype, device=Q.device) if O is None else O
+    torch, dev, where = _torch(), _current_device(), "bra_cross_attend"
+    t, q, k, v, nq, B, keys, stats, n_stats = _derived(p, _cross_derived)
+    q_at, k_at, v_at = _rows_at(Q, "Q", where, t, dev, q), _rows_at(K, "K", where, t, dev, k), _rows_at(V, "V", where, t, dev, v)
+    len_at, mask_at = _cross_mask(key_len, key_mask, where, torch, B, keys, dev)
+    if ws is None:
+        ws = cross_workspace(p, Q.device)
+    if O is None:
+        O = torch.empty(Q.shape, dtype=t, device=Q.device)
+        o_at = O.data_ptr()
+    else:
+        o_at = _at(O, "O", where, t, nq, dev)
     if lse is None and want_lse:
-        lse = torch.empty(p.B, p.heads, p.Nq, dtype=torch.float32, device=Q.device)
-    _check(load_library().bra_cross_attend(ctypes.byref(p), *ins, _tensor(O, "O", where, t, nq, dev),
-                                           _tensor(lse, "lse", where, torch.float32, p.B * p.heads * p.Nq, dev, optional=True),
-                                           _tensor(ws, "ws", where, torch.uint8, ws.numel(), dev), ws.numel(), _stream(stream)), where)
+        lse = torch.empty(stats, dtype=torch.float32, device=Q.device)
+    n_ws = ws.numel()
+    code = (_LIB or load_library()).bra_cross_attend(
+        ctypes.byref(p), q_at, k_at, v_at, len_at, mask_at, o_at, None if lse is None else _at(lse, "lse", where, torch.float32, n_stats, dev),
+        _at(ws, "ws", where, torch.uint8, n_ws, dev), n_ws, _stream(stream))
+    if code:
+        raise BraError(code, where)
     return O, lse
 
 
 def bra_cross_backward(p, Q, K, V, O, lse, dO, key_len=None, key_mask=None, dQ=None, dK=None, dV=None, ws=None, stream=None):
     """bra_cross_backward: -> (dQ, dK, dV)."""
-    torch = _torch()
-    dev, t, where = _current_device(), _tdtype(p), "bra_cross_backward"
-    q, k, v, o = _cross_tokens(p)
-    nq, nk = p.B * p.Nq * q[2], p.B * p.Nk * k[2]
-    ins = [_tensor(Q, "Q", where, t, nq, dev, tokens=q), _tensor(K, "K", where, t, nk, dev, tokens=k),
-           _tensor(V, "V", where, t, nk, dev, tokens=v), *_cross_mask(p, key_len, key_mask, where, dev),
-           _tensor(O, "O", where, t, nq, dev), _tensor(lse, "lse", where, torch.float32, p.B * p.heads * p.Nq, dev),
-           _tensor(dO, "dO", where, t, nq, dev)]
-    ws = cross_workspace(p, Q.device) if ws is None else ws
+    torch, dev, where = _torch(), _current_device(), "bra_cross_backward"
+    t, q, k, v, nq, B, keys, stats, n_stats = _derived(p, _cross_derived)
+    ins = (_rows_at(Q, "Q", where, t, dev, q), _rows_at(K, "K", where, t, dev, k), _rows_at(V, "V", where, t, dev, v),
+           *_cross_mask(key_len, key_mask, where, torch, B, keys, dev), _at(O, "O", where, t, nq, dev),
+           _at(lse, "lse", where, torch.float32, n_stats, dev), _at(dO, "dO", where, t, nq, dev))
+    if ws is None:
+        ws = cross_workspace(p, Q.device)
     dQ = _like(Q, q) if dQ is None else dQ
     dK = _like(K, k) if dK is None else dK
     dV = _like(V, v) if dV is None else dV
-    _check(load_library().bra_cross_backward(ctypes.byref(p), *ins, _tensor(dQ, "dQ", where, t, nq, dev, tokens=q),
-                                             _tensor(dK, "dK", where, t, nk, dev, tokens=k),
-                                             _tensor(dV, "dV", where, t, nk, dev, tokens=v),
-                                             _tensor(ws, "ws", where, torch.uint8, ws.numel(), dev), ws.numel(), _stream(stream)), where)
+    n_ws = ws.numel()
+    code = (_LIB or load_library()).bra_cross_backward(
+        ctypes.byref(p), *ins, _rows_at(dQ, "dQ", where, t, dev, q), _rows_at(dK, "dK", where, t, dev, k), _rows_at(dV, "dV", where, t, dev, v),
+        _at(ws, "ws", where, torch.uint8, n_ws, dev), n_ws, _stream(stream))
+    if code:
+        raise BraError(code, where)
     return dQ, dK, dV
 
 
@@ -490,44 +534,61 @@ def norm_workspace(p: BraNormProblem, device="cuda"):
     return _scratch(norm_workspace_bytes(p), "bra_norm_workspace_bytes", device)
 
 
-def _norm_weights(p, gate, post_w, post_b, w, b, where, dev):
-    f32 = _torch().float32
-    affine = p.C * (p.B if p.per_image else 1)
-    return [_tensor(gate, "gate", where, f32, p.C * (p.B if p.gate == 2 else 1), dev, optional=p.gate == 0),
-            _tensor(post_w, "post_w", where, f32, p.C, dev, optional=True), _tensor(post_b, "post_b", where, f32, p.C, dev, optional=True),
-            _tensor(w, "w", where, f32, affine, dev, optional=True), _tensor(b, "b", where, f32, affine, dev, optional=True)]
+def _norm_derived(p):
+    return _tdtype(p), p.B * p.N * p.C, p.C, p.C * (p.B if p.gate == 2 else 1), p.C * (p.B if p.per_image else 1), p.pre != 0
+
+
+def _weight(t, name, where, numel, dev):
+    return None if t is None else _at(t, name, where, _TORCH.float32, numel, dev)
 
 
 def bra_residual_norm(p, x, y=None, gate=None, post_w=None, post_b=None, w=None, b=None, h=None, n=None, stream=None, want_h=True):
     """bra_residual_norm: x, y -> (h, n): the residual stream behind the block, and what the next block reads."""
-    torch = _torch()
-    dev, t, where, size = _current_device(), _tdtype(p), "bra_residual_norm", p.B * p.N * p.C
-    ins = [_tensor(x, "x", where, t, size, dev), _tensor(y, "y", where, t, size, dev, optional=True),
-           *_norm_weights(p, gate, post_w, post_b, w, b, where, dev)]
-    h = torch.empty_like(x) if h is None and want_h else h
-    n = torch.empty_like(x) if n is None and p.pre else n
-    _check(load_library().bra_residual_norm(ctypes.byref(p), *ins, _tensor(h, "h", where, t, size, dev, optional=True),
-                                            _tensor(n, "n", where, t, size, dev, optional=True), _stream(stream)), where)
+    torch, dev, where = _torch(), _current_device(), "bra_residual_norm"
+    t, size, C, gates, affine, normed = _derived(p, _norm_derived)
+    x_at = _at(x, "x", where, t, size, dev)
+    y_at = None if y is None else _at(y, "y", where, t, size, dev)
+    if h is None and want_h:
+        h = torch.empty_like(x)
+        h_at = h.data_ptr()
+    else:
+        h_at = None if h is None else _at(h, "h", where, t, size, dev)
+    if n is None and normed:
+        n = torch.empty_like(x)
+        n_at = n.data_ptr()
+    else:
+        n_at = None if n is None else _at(n, "n", where, t, size, dev)
+    code = (_LIB or load_library()).bra_residual_norm(
+        ctypes.byref(p), x_at, y_at, _weight(gate, "gate", where, gates, dev), _weight(post_w, "post_w", where, C, dev),
+        _weight(post_b, "post_b", where, C, dev), _weight(w, "w", where, affine, dev), _weight(b, "b", where, affine, dev), h_at, n_at,
+        _stream(stream))
+    if code:
+        raise BraError(code, where)
     return h, n
 
 
 def bra_residual_norm_backward(p, x, y, dh, dn, gate=None, post_w=None, post_b=None, w=None, b=None, dx=None, dy=None, ws=None,
                                stream=None):
     """bra_residual_norm_backward: -> {"dx", "dy", and of the weights that are given "dgate", "d_post_w", "d_post_b", "dw", "db"}."""
-    torch = _torch()
-    dev, t, where, size = _current_device(), _tdtype(p), "bra_residual_norm_backward", p.B * p.N * p.C
-    weights = _norm_weights(p, gate, post_w, post_b, w, b, where, dev)
-    ins = [_tensor(x, "x", where, t, size, dev), _tensor(y, "y", where, t, size, dev, optional=True), *weights[:4],
-           _tensor(dh, "dh", where, t, size, dev, optional=True), _tensor(dn, "dn", where, t, size, dev, optional=True)]
-    ws = norm_workspace(p, x.device) if ws is None else ws
+    torch, dev, where = _torch(), _current_device(), "bra_residual_norm_backward"
+    t, size, C, gates, affine, _ = _derived(p, _norm_derived)
+    ins = (_at(x, "x", where, t, size, dev), None if y is None else _at(y, "y", where, t, size, dev), _weight(gate, "gate", where, gates, dev),
+           _weight(post_w, "post_w", where, C, dev), _weight(post_b, "post_b", where, C, dev), _weight(w, "w", where, affine, dev),
+           None if dh is None else _at(dh, "dh", where, t, size, dev), None if dn is None else _at(dn, "dn", where, t, size, dev))
+    _weight(b, "b", where, affine, dev)
+    if ws is None:
+        ws = norm_workspace(p, x.device)
     out = {"dx": torch.empty_like(x) if dx is None else dx}
     if y is not None:
         out["dy"] = torch.empty_like(y) if dy is None else dy
     for name, weight in (("dgate", gate), ("d_post_w", post_w), ("d_post_b", post_b), ("dw", w), ("db", b)):
         if weight is not None:
             out[name] = torch.empty_like(weight)
-    _check(load_library().bra_residual_norm_backward(
-        ctypes.byref(p), *ins, _tensor(out["dx"], "dx", where, t, size, dev), _tensor(out.get("dy"), "dy", where, t, size, dev, optional=True),
+    n_ws = ws.numel()
+    code = (_LIB or load_library()).bra_residual_norm_backward(
+        ctypes.byref(p), *ins, _at(out["dx"], "dx", where, t, size, dev), None if y is None else _at(out["dy"], "dy", where, t, size, dev),
         *(_ptr(out.get(name)) for name in ("dgate", "d_post_w", "d_post_b", "dw", "db")),
-        _tensor(ws, "ws", where, torch.uint8, ws.numel(), dev), ws.numel(), _stream(stream)), where)
+        _at(ws, "ws", where, torch.uint8, n_ws, dev), n_ws, _stream(stream))
+    if code:
+        raise BraError(code, where)
     return out
