@@ -36,6 +36,7 @@ struct NormArgs {
     int gate_image, affine_image;           // [B, C] rather than [C]
     int pre, post;
     float eps, alpha;
+    int ring_slots, ring_pitch;             // of rows that are a CTA's
     int sums;                               // which sums are wanted, SUM_* bits
     long long slots;
 };
@@ -87,42 +88,47 @@ __device__ __forceinline__ void widen(const uint32_t (&w)[4], Eight& f) {
 // How far rows are read ahead: through a ring in shared memory whose 16- or 4-byte slots are each one thread's own, so that neither
 // registers nor barriers are spent on rows in flight; one slot more than rows in flight, so that none is written that was read in the
 // same round.  Rows of bf16 that start on two bytes cannot be copied so (four at least) and go through registers, one row ahead.
-// DEPTH: rows in flight, as many as shared memory has room for; 0: rows are read when it is their turn.
-template <typename T, bool VECD, int TENSORS, int DEPTH>
+// DEPTH: rounds in flight.
+template <typename T, bool VECD, int TENSORS, int DEPTH, int R>
 struct Ahead {
-    static constexpr bool RING = DEPTH > 0 && (VECD || sizeof(T) == 4);
-    static constexpr int ROWS = RING || DEPTH == 0 ? DEPTH : 1;
+    static constexpr bool RING = VECD || sizeof(T) == 4;
+    static constexpr int ROWS = RING ? DEPTH : 1;
     static constexpr int CHUNKS = VECD ? NORM_E * (int)sizeof(T) / 16 : NORM_E, CHUNK = VECD ? 16 : 4;
-    static constexpr size_t bytes(int threads) { return RING ? (size_t)(DEPTH + 1) * TENSORS * NORM_E * sizeof(T) * threads : 0; }
-    T raw[RING || DEPTH == 0 ? 1 : TENSORS][NORM_E];
+    static constexpr size_t bytes(int threads) { return RING ? (size_t)(DEPTH + 1) * TENSORS * R * NORM_E * sizeof(T) * threads : 0; }
+    T raw[RING ? 1 : TENSORS * R][NORM_E];
     const T* row[TENSORS];                  // of the row that is fetched next, at this thread's first channel; null: no such tensor
     uint32_t base, pitch;                   // this thread's first slot, bytes between its chunks
     uint32_t get = 0, put = 0;              // offsets of the rows that are read and fetched next
     __device__ __forceinline__ void restart() { get = put; }         // nothing that was fetched is left to read
     __device__ __forceinline__ explicit Ahead(const void* smem) : base(ptx::smem_u32(smem) + threadIdx.x * CHUNK), pitch(blockDim.x * CHUNK) {}
     __device__ __forceinline__ uint32_t step(uint32_t at) const {
-        at += TENSORS * CHUNKS * pitch;
-        return at == (DEPTH + 1) * TENSORS * CHUNKS * pitch ? 0 : at;
+        at += TENSORS * R * CHUNKS * pitch;
+        return at == (DEPTH + 1) * TENSORS * R * CHUNKS * pitch ? 0 : at;
     }
-    // fetches a row of every tensor (live: it exists) and moves on by `stride` elements
-    __device__ __forceinline__ void fetch(bool live, long long stride, const Cols<VECD>& c) {
+    // fetches R rows of every tensor, `between` elements apart, of which those with a number below `end` exist (first: of the first one,
+    // then every `groups`th), and moves on by R of them
+    __device__ __forceinline__ void fetch(int first, int groups, int end, int between, const Cols<VECD>& c) {
 #pragma unroll
         for (int k = 0; k < TENSORS; ++k) {
             if (!row[k]) continue;
-            if (live) {
-                if constexpr (RING) {
-                    const uint32_t to = base + put + k * CHUNKS * pitch;
 #pragma unroll
-                    for (int j = 0; j < CHUNKS; ++j) {
-                        if constexpr (VECD) ptx::cp_async_16(to + j * pitch, c.any ? row[k] + j * (16 / (int)sizeof(T)) : row[k] - c.at(0), c.any ? 16 : 0);
-                        else ptx::cp_async_4(to + j * pitch, c.has(j) ? row[k] + j * c.group : row[k] - c.t, c.has(j) ? 4 : 0);
+            for (int q = 0; q < R; ++q) {
+                const T* from = row[k] + q * between;
+                if (first + q * groups < end) {
+                    if constexpr (RING) {
+                        const uint32_t to = base + put + (k * R + q) * CHUNKS * pitch;
+#pragma unroll
+                        for (int j = 0; j < CHUNKS; ++j) {
+                            if constexpr (VECD) ptx::cp_async_16(to + j * pitch, c.any ? from + j * (16 / (int)sizeof(T)) : from - c.at(0), c.any ? 16 : 0);
+                            else ptx::cp_async_4(to + j * pitch, c.has(j) ? from + j * c.group : from - c.t, c.has(j) ? 4 : 0);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < NORM_E; ++j) raw[k * R + q][j] = c.has(j) ? from[j * c.group] : T(0.f);
                     }
-                } else if constexpr (DEPTH > 0) {
-#pragma unroll
-                    for (int j = 0; j < NORM_E; ++j) raw[k][j] = c.has(j) ? row[k][j * c.group] : T(0.f);
                 }
             }
-            row[k] += stride;
+            row[k] += (long long)R * between;
         }
         if (RING) {
             ptx::cp_async_commit();
@@ -130,19 +136,9 @@ struct Ahead {
         }
     }
     __device__ __forceinline__ void arrived() { if constexpr (RING) ptx::cp_async_wait<DEPTH - 1>(); }
-    __device__ __forceinline__ void read(int tensor, Eight& f, const Cols<VECD>& c) const {
-        if constexpr (DEPTH == 0) {
-            float v[NORM_E] = {};
-            if constexpr (VECD) {
-                if (c.any) load_row<NORM_E>(row[tensor], v);
-            } else {
-#pragma unroll
-                for (int j = 0; j < NORM_E; ++j) if (c.has(j)) v[j] = (float)row[tensor][j * c.group];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) f.v[i] = make_float2(v[2 * i], v[2 * i + 1]);
-        } else if constexpr (RING) {
-            const uint32_t from = base + get + tensor * CHUNKS * pitch;
+    __device__ __forceinline__ void read(int tensor, int q, int between, Eight& f, const Cols<VECD>& c) const {
+        if constexpr (RING) {
+            const uint32_t from = base + get + (tensor * R + q) * CHUNKS * pitch;
             if constexpr (VECD && sizeof(T) == 2) {
                 const float4 v = ptx::lds_f32x4(from);
                 widen({__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)}, f);
@@ -159,15 +155,120 @@ struct Ahead {
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) f.v[i] = make_float2(__bfloat162float(raw[tensor][2 * i]), __bfloat162float(raw[tensor][2 * i + 1]));
+            for (int i = 0; i < 4; ++i) f.v[i] = make_float2(__bfloat162float(raw[tensor * R + q][2 * i]), __bfloat162float(raw[tensor * R + q][2 * i + 1]));
         }
     }
     __device__ __forceinline__ void next() { if (RING) get = step(get); }
 };
 
-// 4096 channels of fp32 backwards: 82 KB of sums and a ring of 131 KB; 8192: 164 KB of sums
-__host__ __device__ constexpr int forward_depth(int threads) { return threads <= 512 ? 3 : 2; }
-__host__ __device__ constexpr int backward_depth(int threads) { return threads <= 128 ? 3 : threads <= 512 ? 1 : 0; }
+// The same for rows that are a CTA's: R rows of a tensor are one stretch of memory, which one thread copies (bulk copies, a barrier a
+// slot), whatever their alignment: a stretch is copied from the 16-byte boundary before it to the one behind it, so the row starts
+// `skew` bytes into its slot.  The tensor's own end need not be such a boundary: rows that reach into the last 16 bytes are read where
+// they are, and so are all rows where shared memory has no room for a slot, or if a wait should give up.
+constexpr int NORM_SLOTS = 4;
+template <typename T, bool VECD, int TENSORS, int R>
+struct Stretch {
+    const T* tensor[TENSORS];               // whole ones; null: no such tensor
+    uint64_t* full;                         // [slots]
+    uint32_t base;
+    int slots, pitch, C;                    // pitch: bytes of a tensor's part of a slot
+    long long last_byte;                    // bytes of a tensor that may be copied
+    uint32_t count = 0, asked = 0;          // units read and asked for
+    int row = 0, end = 0;                   // of the unit that is read next, and the last row of this stretch of rows, plus one
+    bool direct = false;
+    __device__ __forceinline__ Stretch(const NormArgs& a, uint32_t smem, uint64_t* bars)
+        : full(bars), base(smem), slots(a.ring_slots), pitch(a.ring_pitch), C(a.C), last_byte(a.rows * a.C * (long long)sizeof(T) / 16 * 16) {
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < NORM_SLOTS; ++i) ptx::mbar_init(full + i, 1);
+            ptx::fence_mbar_init();
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ long long byte_of(int r) const { return (long long)r * C * (int)sizeof(T); }
+    __device__ __forceinline__ bool copied(int first) const {
+        return slots > 0 && (byte_of(min(first + R, end)) + 15) / 16 * 16 <= last_byte;
+    }
+    __device__ __forceinline__ void ask(int first) {                   // one thread
+        if (first >= end) return;
+        const uint32_t s = asked % slots;
+        ++asked;
+        if (!copied(first)) { ptx::mbar_arrive(full + s); return; }
+        const long long from = byte_of(first) / 16 * 16, to = (byte_of(min(first + R, end)) + 15) / 16 * 16;
+        int n = 0;
+#pragma unroll
+        for (int k = 0; k < TENSORS; ++k) n += tensor[k] != nullptr;
+        ptx::mbar_expect_tx(full + s, (uint32_t)(to - from) * n);
+#pragma unroll
+        for (int k = 0; k < TENSORS; ++k)
+            if (tensor[k]) ptx::bulk_load(base + (s * TENSORS + k) * pitch, reinterpret_cast<const char*>(tensor[k]) + from, (uint32_t)(to - from), full + s);
+    }
+    // rows first .. end_ - 1, from now on
+    __device__ __forceinline__ void start(int first, int end_) {
+        row = first;
+        end = end_;
+        if (threadIdx.x == 0)
+            for (int i = 0; i < slots; ++i) ask(first + i * R);
+    }
+    __device__ __forceinline__ void arrived() {
+        direct = !copied(row);
+        if (slots > 0) {
+            if (!ptx::mbar_try_wait(full + count % slots, (count / slots) & 1)) direct = !ptx::mbar_wait(full + count % slots, (count / slots) & 1) || direct;
+        }
+    }
+    __device__ __forceinline__ void read(int tensor_at, int q, Eight& f, const Cols<VECD>& c) const {
+        float v[NORM_E] = {};
+        if (direct) {
+            const T* from = tensor[tensor_at] + (long long)min(row + q, end - 1) * C;
+            if constexpr (VECD) {
+                if (c.any) load_row<NORM_E>(from + c.at(0), v);
+            } else {
+#pragma unroll
+                for (int j = 0; j < NORM_E; ++j) if (c.has(j)) v[j] = (float)from[c.at(j)];
+            }
+        } else {
+            const uint32_t at = base + ((count % slots) * TENSORS + tensor_at) * pitch + (uint32_t)(byte_of(row) & 15) + q * C * (int)sizeof(T) + c.at(0) * (int)sizeof(T);
+            if constexpr (VECD && sizeof(T) == 2) {
+                float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (c.any) t = ptx::lds_f32x4(at);
+                widen({__float_as_uint(t.x), __float_as_uint(t.y), __float_as_uint(t.z), __float_as_uint(t.w)}, f);
+                return;
+            } else if constexpr (VECD) {
+                if (c.any) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float4 t = ptx::lds_f32x4(at + 16 * k);
+                        v[4 * k] = t.x; v[4 * k + 1] = t.y; v[4 * k + 2] = t.z; v[4 * k + 3] = t.w;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < NORM_E; ++j)
+                    if (c.has(j)) {
+                        if constexpr (sizeof(T) == 4) v[j] = ptx::lds_f32(at + j * c.group * 4);
+                        else v[j] = __uint_as_float((uint32_t)ptx::lds_u16(at + j * c.group * 2) << 16);
+                    }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f.v[i] = make_float2(v[2 * i], v[2 * i + 1]);
+    }
+    // behind a barrier that all threads met after their reads: the slot takes the unit `slots` further on
+    __device__ __forceinline__ void next() {
+        if (threadIdx.x == 0 && slots > 0) ask(row + slots * R);
+        row += R;
+        ++count;
+    }
+};
+
+// Which of the two: stretches where a thread would copy its channels one by one, or has no registers to address them by.  Measured
+// (B200, us, forward + backward, stretches / slots of threads): 8 x 1024 x 768 bf16 52 + 92 / 20 + 36, x 4096 59 + 155 / 46 + 107; 765 bf16 21 + 38 /
+// 21 + 47, 5001 fp32 181 + 470 / 205 + 524, 5000 fp32 154 + 383 / 188 + 378.
+template <bool VECD, int G, int THREADS>
+constexpr bool STRETCHES = G == 0 && (!VECD || THREADS > 512);
+// rounds in flight of the slots of threads
+__host__ __device__ constexpr int forward_depth(int threads, int rows) { return rows == 1 ? 3 : 2; }
+__host__ __device__ constexpr int backward_rows(int threads, bool post) { return threads <= 128 && !post ? 2 : 1; }
+__host__ __device__ constexpr int backward_depth(int threads, int rows) { return threads > 128 ? 1 : rows == 1 ? 3 : 2; }
 
 template <typename T, bool VECD>
 __device__ __forceinline__ void put(T* row, const Eight& f, const Cols<VECD>& c) {
@@ -207,123 +308,144 @@ __device__ __forceinline__ void weights(const float* p, float none, Eight& f, co
 __device__ __forceinline__ const float* row_of(const float* p, long long off) { return p ? p + off : nullptr; }
 
 // ---------------------------------------------------------------- sums over a row
-// G: lanes of a row; 0: the row is the CTA's.  The buffers of two consecutive sums are different ones, so that one barrier a sum
-// is enough.
+// G: lanes of a row; 0: the row is the CTA's.  K sums at once: their exchanges overlap and share a barrier.  The buffers of two
+// consecutive calls are different ones, so that one barrier a call is enough.
+constexpr int SUMS_AT_ONCE = 4;
 template <int G>
 struct RowSum {
-    float2 (*cross)[32];                    // [2][warps]
+    float (*cross)[32][SUMS_AT_ONCE];       // [2][warps]
     int turn = 0;
-    __device__ __forceinline__ float2 of(float a, float b) {
+    template <int K>
+    __device__ __forceinline__ void of(float (&a)[K]) {
 #pragma unroll
-        for (int o = (G ? G : 32) >> 1; o; o >>= 1) {
-            a += __shfl_xor_sync(0xffffffffu, a, o);
-            b += __shfl_xor_sync(0xffffffffu, b, o);
-        }
+        for (int o = (G ? G : 32) >> 1; o; o >>= 1)
+#pragma unroll
+            for (int k = 0; k < K; ++k) a[k] += __shfl_xor_sync(0xffffffffu, a[k], o);
         if (G == 0) {
             const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-            if (lane == 0) cross[turn][warp] = make_float2(a, b);
+            if (lane == 0)
+#pragma unroll
+                for (int k = 0; k < K; ++k) cross[turn][warp][k] = a[k];
             __syncthreads();
             if (warps <= 4) {
-                float2 s = cross[turn][0];
-                for (int w = 1; w < warps; ++w) s = __fadd2_rn(s, cross[turn][w]);
-                a = s.x; b = s.y;
-            } else {
-                const float2 s = lane < warps ? cross[turn][lane] : make_float2(0.f, 0.f);
-                a = s.x; b = s.y;
 #pragma unroll
-                for (int o = 16; o; o >>= 1) {
-                    a += __shfl_xor_sync(0xffffffffu, a, o);
-                    b += __shfl_xor_sync(0xffffffffu, b, o);
-                }
+                for (int k = 0; k < K; ++k) a[k] = cross[turn][0][k];
+                for (int w = 1; w < warps; ++w)
+#pragma unroll
+                    for (int k = 0; k < K; ++k) a[k] += cross[turn][w][k];
+            } else {
+#pragma unroll
+                for (int k = 0; k < K; ++k) a[k] = lane < warps ? cross[turn][lane][k] : 0.f;
+#pragma unroll
+                for (int o = 16; o; o >>= 1)
+#pragma unroll
+                    for (int k = 0; k < K; ++k) a[k] += __shfl_xor_sync(0xffffffffu, a[k], o);
             }
             turn ^= 1;
         }
-        return make_float2(a, b);
-    }
-    __device__ __forceinline__ float of(float a) {
-#pragma unroll
-        for (int o = (G ? G : 32) >> 1; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-        if (G == 0) {
-            const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-            if (lane == 0) cross[turn][warp].x = a;
-            __syncthreads();
-            if (warps <= 4) {
-                a = cross[turn][0].x;
-                for (int w = 1; w < warps; ++w) a += cross[turn][w].x;
-            } else {
-                a = lane < warps ? cross[turn][lane].x : 0.f;
-#pragma unroll
-                for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-            }
-            turn ^= 1;
-        }
-        return a;
     }
 };
 
-// v becomes its normalised form; the factor is returned.  Channels that do not exist hold zeros and keep them.
-template <int G, bool VECD>
-__device__ __forceinline__ float normalise(int kind, Eight& v, const Cols<VECD>& c, float eps, float per_channel, RowSum<G>& sum) {
+// R rows become their normalised forms; their factors go to r.  Channels that do not exist hold zeros and keep them.
+template <int G, int R, bool VECD>
+__device__ __forceinline__ void normalise(int kind, Eight (&v)[R], float (&r)[R], const Cols<VECD>& c, float eps, float per_channel, RowSum<G>& sum) {
+    float s[R];
     if (kind == BRA_NORM_LAYER) {
-        const float mean = sum.of(total(v)) * per_channel;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v.v[i] = __fadd2_rn(v.v[i], c.only(-mean, i));
+        for (int q = 0; q < R; ++q) s[q] = total(v[q]);
+        sum.of(s);
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            const float mean = s[q] * per_channel;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[q].v[i] = __fadd2_rn(v[q].v[i], c.only(-mean, i));
+        }
     }
-    const float r = rsqrtf(fmaf(sum.of(dot(v, v)), per_channel, eps));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v.v[i] = __fmul2_rn(v.v[i], both(r));
-    return r;
+    for (int q = 0; q < R; ++q) s[q] = dot(v[q], v[q]);
+    sum.of(s);
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+        r[q] = rsqrtf(fmaf(s[q], per_channel, eps));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[q].v[i] = __fmul2_rn(v[q].v[i], both(r[q]));
+    }
 }
 
-// g becomes the gradient of the row whose normalised form hat had the gradient g: r (g - hat mean(g hat) [- mean(g)])
-template <int G, bool VECD>
-__device__ __forceinline__ void normalise_back(int kind, Eight& g, const Eight& hat, float r, const Cols<VECD>& c, float per_channel, RowSum<G>& sum) {
-    float2 m = make_float2(0.f, 0.f);
-    if (kind == BRA_NORM_LAYER) m = sum.of(dot(g, hat), total(g));
-    else m.x = sum.of(dot(g, hat));
-    const float along = -r * (m.x * per_channel), mean = -r * (m.y * per_channel);
+// g becomes the gradient of the rows whose normalised forms hat had the gradients g: r (g - hat mean(g hat) [- mean(g)])
+template <int G, int R, bool VECD>
+__device__ __forceinline__ void normalise_back(int kind, Eight (&g)[R], const Eight (&hat)[R], const float (&r)[R], const Cols<VECD>& c, float per_channel,
+                                               RowSum<G>& sum) {
+    float m[2 * R];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) g.v[i] = __ffma2_rn(g.v[i], both(r), __ffma2_rn(hat.v[i], both(along), c.only(mean, i)));
+    for (int q = 0; q < R; ++q) {
+        m[q] = dot(g[q], hat[q]);
+        m[R + q] = kind == BRA_NORM_LAYER ? total(g[q]) : 0.f;
+    }
+    sum.of(m);
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+        const float along = -r[q] * (m[q] * per_channel), mean = -r[q] * (m[R + q] * per_channel);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g[q].v[i] = __ffma2_rn(g[q].v[i], both(r[q]), __ffma2_rn(hat[q].v[i], both(along), c.only(mean, i)));
+    }
 }
 
 // ---------------------------------------------------------------- forward
-// A CTA's groups take the rows of its run in turn.  All groups make the same number of rounds (those without a row compute on what
-// the ring holds and store nothing), so that the shuffles and barriers of the sums are met by every thread.
+// A CTA's groups take the rows of its run in turn, R rows a round.  All groups make the same number of rounds (those without a row
+// compute on what the ring holds and store nothing), so that the shuffles and barriers of the sums are met by every thread.
 // THREADS: the most a CTA has.  Above 512 a thread has 64 registers: weights are read where they are used, row by row.
-template <typename T, bool VECD, int G, bool POST, int THREADS>
+// R: two rows are two independent chains of exchanges and sums (one: 310 instructions a round of four 64-channel rows, 0.62 of them
+// issued per cycle and scheduler).
+__host__ __device__ constexpr int forward_rows(int threads) { return threads <= 128 ? 2 : 1; }
+template <typename T, bool VECD, int G, bool POST, int THREADS, int R>
 __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormArgs a) {
-    constexpr bool KEEP = THREADS <= 512;
-    __shared__ float2 cross[2][32];
+    constexpr bool KEEP = THREADS <= 512, STRETCH = STRETCHES<VECD, G, THREADS>;
+    __shared__ float cross[2][32][SUMS_AT_ONCE];
     extern __shared__ __align__(16) char ring[];
-    const int groups = G ? THREADS / (G ? G : 1) : 1;
+    constexpr int GROUPS = G ? THREADS / (G ? G : 1) : 1;
     const int mine = G ? threadIdx.x / (G ? G : 1) : 0;
     const Cols<VECD> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
     RowSum<G> sum{cross};
     const int first = (int)(blockIdx.x * (long long)a.run), end = (int)min((long long)first + a.run, a.rows);
     const float per_channel = 1.f / (float)a.C;
     const bool has_y = a.y != nullptr;
-    const long long start = (long long)(first + mine) * a.C, stride = (long long)groups * a.C;
+    const long long start = (long long)(first + mine) * a.C;
+    const int between = GROUPS * a.C;
 
-    Ahead<T, VECD, 2, forward_depth(THREADS)> in(ring);
-    in.row[0] = static_cast<const T*>(a.x) + start + c.at(0);
-    in.row[1] = has_y ? static_cast<const T*>(a.y) + start + c.at(0) : nullptr;
+    // rows of lanes go through slots of threads, rows of a CTA through slots of its own
+    __shared__ uint64_t full[NORM_SLOTS];
+    auto rows_in = [&] {
+        if constexpr (!STRETCH) return Ahead<T, VECD, 2, forward_depth(THREADS, R), R>(ring);
+        else return Stretch<T, VECD, 2, R>(a, ptx::smem_u32(ring), full);
+    };
+    auto in = rows_in();
+    if constexpr (!STRETCH) {
+        in.row[0] = static_cast<const T*>(a.x) + start + c.at(0);
+        in.row[1] = has_y ? static_cast<const T*>(a.y) + start + c.at(0) : nullptr;
+    } else {
+        in.tensor[0] = static_cast<const T*>(a.x);
+        in.tensor[1] = static_cast<const T*>(a.y);
+        in.start(first, end);
+    }
     T* h = a.h ? static_cast<T*>(a.h) + start : nullptr;
     T* n = a.n ? static_cast<T*>(a.n) + start : nullptr;
     int ask = first + mine;
+    if constexpr (!STRETCH) {
 #pragma unroll
-    for (int k = 0; k < in.ROWS; ++k, ask += groups) in.fetch(ask < end, stride, c);
+        for (int k = 0; k < in.ROWS; ++k, ask += R * GROUPS) in.fetch(ask, GROUPS, end, between, c);
+    }
     const bool per_image = a.gate_image || a.affine_image;
-    int image_end = first + mine;                             // rows before it have the weights that are held
+    // rows before it have the weights that are held; with weights of images a round ends with its image (R = 1 then)
+    int image_end = first + mine;
     Eight gate, pw, pb, w, b;
     const float *gate_p = a.gate, *w_p = a.w, *b_p = a.b;
     if (POST && KEEP) {
         weights<VECD>(a.post_w, 1.f, pw, c);
         weights<VECD>(a.post_b, 0.f, pb, c);
     }
-    for (int row0 = first; row0 < end; row0 += groups) {
-        const int row = row0 + mine;
-        const bool live = row < end;
-        if (row >= image_end && live) {
+    for (int row = first + mine; row - mine < end; row += R * GROUPS) {
+        if (row >= image_end && row < end) {
             const int image = per_image ? row / a.N : 0;
             gate_p = row_of(a.gate, a.gate_image ? (long long)image * a.C : 0);
             w_p = row_of(a.w, a.affine_image ? (long long)image * a.C : 0);
@@ -335,55 +457,90 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormArgs a)
             }
             image_end = per_image ? (int)min((long long)(image + 1) * a.N, (long long)end) : end;
         }
-        Eight v, u;
+        Eight v[R], u[R];
+        float r[R];
         in.arrived();
-        in.read(0, v, c);
-        if (has_y) in.read(1, u, c);
-        in.fetch(ask < end, stride, c);
-        ask += groups;
-        in.next();
+        if constexpr (!STRETCH) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v.v[i] = __fmul2_rn(v.v[i], both(a.alpha));
+            for (int q = 0; q < R; ++q) {
+                in.read(0, q, between, v[q], c);
+                if (has_y) in.read(1, q, between, u[q], c);
+            }
+            in.fetch(ask, GROUPS, end, between, c);
+            ask += R * GROUPS;
+            in.next();
+        } else {
+#pragma unroll
+            for (int q = 0; q < R; ++q) {
+                in.read(0, q, v[q], c);
+                if (has_y) in.read(1, q, u[q], c);
+            }
+            if (!POST && !n) __syncthreads();                  // else the sums' barriers say that all have read
+        }
+#pragma unroll
+        for (int q = 0; q < R; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[q].v[i] = __fmul2_rn(v[q].v[i], both(a.alpha));
         if (has_y) {
             if (POST) {
-                normalise<G>(a.post, u, c, a.eps, per_channel, sum);
+                normalise<G>(a.post, u, r, c, a.eps, per_channel, sum);
                 if (!KEEP) { weights<VECD>(a.post_w, 1.f, pw, c); weights<VECD>(a.post_b, 0.f, pb, c); }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) u.v[i] = __ffma2_rn(u.v[i], pw.v[i], pb.v[i]);
+                for (int q = 0; q < R; ++q)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) u[q].v[i] = __ffma2_rn(u[q].v[i], pw.v[i], pb.v[i]);
             }
             if (!KEEP) weights<VECD>(gate_p, 1.f, gate, c);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v.v[i] = __ffma2_rn(gate.v[i], u.v[i], v.v[i]);
+            for (int q = 0; q < R; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[q].v[i] = __ffma2_rn(gate.v[i], u[q].v[i], v[q].v[i]);
         }
         if (h) {
-            if (live) put<T, VECD>(h, v, c);
-            h += stride;
+#pragma unroll
+            for (int q = 0; q < R; ++q)
+                if (row + q * GROUPS < end) put<T, VECD>(h + q * between, v[q], c);
+            h += (long long)R * between;
         }
         if (n) {
-            normalise<G>(a.pre, v, c, a.eps, per_channel, sum);
+            normalise<G>(a.pre, v, r, c, a.eps, per_channel, sum);
             if (!KEEP) { weights<VECD>(w_p, 1.f, w, c); weights<VECD>(b_p, 0.f, b, c); }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v.v[i] = __ffma2_rn(v.v[i], w.v[i], b.v[i]);
-            if (live) put<T, VECD>(n, v, c);
-            n += stride;
+            for (int q = 0; q < R; ++q) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[q].v[i] = __ffma2_rn(v[q].v[i], w.v[i], b.v[i]);
+                if (row + q * GROUPS < end) put<T, VECD>(n + q * between, v[q], c);
+            }
+            n += (long long)R * between;
         }
+        if constexpr (STRETCH) in.next();
     }
 }
 
 // ---------------------------------------------------------------- backward
 // THREADS 128: the sums over tokens stay in registers, and so do the weights.  More (long rows, whose CTAs would have no registers
 // left): the sums are in shared memory, each word its thread's own, and the weights are read again for every row.
-template <typename T, bool VECD, int G, bool POST, int THREADS>
+template <typename T, bool VECD, int G, bool POST, int THREADS, int R>
 __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a) {
-    constexpr bool KEEP = THREADS == 128;
-    __shared__ float2 cross[2][32];
+    constexpr bool KEEP = THREADS == 128, STRETCH = STRETCHES<VECD, G, THREADS>;
+    __shared__ float cross[2][32][SUMS_AT_ONCE];
     // !KEEP: [SUMS][E][threads]; KEEP and several groups: [E][threads], to join the groups; then the ring of rows
     extern __shared__ __align__(16) float sums_sh[];
-    const int groups = G ? THREADS / (G ? G : 1) : 1;
+    constexpr int GROUPS = G ? THREADS / (G ? G : 1) : 1;
     const int mine = G ? threadIdx.x / (G ? G : 1) : 0;
     const Cols<VECD> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
     RowSum<G> sum{cross};
-    Ahead<T, VECD, 4, backward_depth(THREADS)> in(sums_sh + NORM_E * blockDim.x * (KEEP ? (G ? 1 : 0) : SUMS));
+    __shared__ uint64_t full[NORM_SLOTS];
+    auto rows_in = [&] {
+        float* ring = sums_sh + NORM_E * blockDim.x * (KEEP ? (G ? 1 : 0) : SUMS);
+        if constexpr (!STRETCH) return Ahead<T, VECD, 4, backward_depth(THREADS, R), R>(ring);
+        else return Stretch<T, VECD, 4, R>(a, ptx::smem_u32(ring), full);
+    };
+    auto in = rows_in();
+    if constexpr (STRETCH) {
+        in.tensor[0] = static_cast<const T*>(a.x); in.tensor[1] = static_cast<const T*>(a.y);
+        in.tensor[2] = static_cast<const T*>(a.dh); in.tensor[3] = static_cast<const T*>(a.dn);
+    }
     const bool has_y = a.y != nullptr, has_n = a.dn != nullptr;
     const int first = (int)(blockIdx.x * (long long)a.run), last = (int)min((long long)first + a.run, a.rows) - 1;
     const float per_channel = 1.f / (float)a.C;
@@ -431,7 +588,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     t.v[i] = both(0.f);
-                    for (int g = 0; g < groups; ++g) t.v[i] = __fadd2_rn(t.v[i], join[i * THREADS + g * G + threadIdx.x]);
+                    for (int g = 0; g < GROUPS; ++g) t.v[i] = __fadd2_rn(t.v[i], join[i * THREADS + g * G + threadIdx.x]);
                 }
             }
         }
@@ -456,82 +613,119 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a
             weights<VECD>(w_p, 1.f, w, c);
             if (POST) { weights<VECD>(a.post_w, 1.f, pw, c); weights<VECD>(a.post_b, 0.f, pb, c); }
         }
-        const long long start = (long long)(begin + mine) * a.C, stride = (long long)groups * a.C;
+        const long long start = (long long)(begin + mine) * a.C;
+        const int between = GROUPS * a.C;
         auto from = [&](const void* p) { return p ? static_cast<const T*>(p) + start + c.at(0) : nullptr; };
-        in.row[0] = from(a.x); in.row[1] = from(a.y); in.row[2] = from(a.dh); in.row[3] = from(a.dn);
+        if constexpr (!STRETCH) { in.row[0] = from(a.x); in.row[1] = from(a.y); in.row[2] = from(a.dh); in.row[3] = from(a.dn); }
         T* dx = static_cast<T*>(a.dx) + start;
         T* dy = has_y ? static_cast<T*>(a.dy) + start : nullptr;
         int ask = begin + mine;
-        in.restart();
+        if constexpr (!STRETCH) {
+            in.restart();
 #pragma unroll
-        for (int k = 0; k < in.ROWS; ++k, ask += groups) in.fetch(ask <= end, stride, c);
-        for (int row0 = begin; row0 <= end; row0 += groups) {
-            const bool live = row0 + mine <= end;
-            Eight v, u, g, d;
+            for (int k = 0; k < in.ROWS; ++k, ask += R * GROUPS) in.fetch(ask, GROUPS, end + 1, between, c);
+        } else {
+            in.start(begin, end + 1);
+        }
+        for (int row = begin + mine; row - mine <= end; row += R * GROUPS) {
+            Eight v[R], u[R], g[R], d[R];
+            float r[R], u_factor[R];
             in.arrived();
-            in.read(0, v, c);
-            if (has_y) in.read(1, u, c);
-            if (a.dh) in.read(2, d, c);
-            else d.fill(0.f);
-            if (has_n) in.read(3, g, c);
-            in.fetch(ask <= end, stride, c);
-            ask += groups;
-            in.next();
+            if constexpr (!STRETCH) {
+#pragma unroll
+                for (int q = 0; q < R; ++q) {
+                    in.read(0, q, between, v[q], c);
+                    if (has_y) in.read(1, q, between, u[q], c);
+                    if (a.dh) in.read(2, q, between, d[q], c);
+                    else d[q].fill(0.f);
+                    if (has_n) in.read(3, q, between, g[q], c);
+                }
+                in.fetch(ask, GROUPS, end + 1, between, c);
+                ask += R * GROUPS;
+                in.next();
+            } else {
+#pragma unroll
+                for (int q = 0; q < R; ++q) {
+                    in.read(0, q, v[q], c);
+                    if (has_y) in.read(1, q, u[q], c);
+                    if (a.dh) in.read(2, q, d[q], c);
+                    else d[q].fill(0.f);
+                    if (has_n) in.read(3, q, g[q], c);
+                }
+                if (!POST && !has_n) __syncthreads();          // else the sums' barriers say that all have read
+            }
             // !KEEP: the weights, as they are used
             auto post_weights = [&] { if (!KEEP && POST) { weights<VECD>(a.post_w, 1.f, pw, c); weights<VECD>(a.post_b, 0.f, pb, c); } };
-            float u_factor = 0.f;
+            auto yy = [&](int q, int i) { return POST ? __ffma2_rn(u[q].v[i], pw.v[i], pb.v[i]) : u[q].v[i]; };
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v.v[i] = __fmul2_rn(v.v[i], both(a.alpha));
+            for (int q = 0; q < R; ++q)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[q].v[i] = __fmul2_rn(v[q].v[i], both(a.alpha));
             if (has_y) {
-                if (POST) u_factor = normalise<G>(a.post, u, c, a.eps, per_channel, sum);
+                if (POST) normalise<G>(a.post, u, u_factor, c, a.eps, per_channel, sum);
                 post_weights();
                 if (!KEEP) weights<VECD>(gate_p, 1.f, gate, c);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v.v[i] = __ffma2_rn(gate.v[i], POST ? __ffma2_rn(u.v[i], pw.v[i], pb.v[i]) : u.v[i], v.v[i]);
+                for (int q = 0; q < R; ++q)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[q].v[i] = __ffma2_rn(gate.v[i], yy(q, i), v[q].v[i]);
             }
             if (has_n) {
-                const float r = normalise<G>(a.pre, v, c, a.eps, per_channel, sum);
+                normalise<G>(a.pre, v, r, c, a.eps, per_channel, sum);
                 if (!KEEP) weights<VECD>(w_p, 1.f, w, c);
-                if (live) {
-                    add(SUM_W, g, v);
-                    add1(SUM_B, g);
-                }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) g.v[i] = __fmul2_rn(g.v[i], w.v[i]);
+                for (int q = 0; q < R; ++q) {
+                    if (row + q * GROUPS <= end) {
+                        add(SUM_W, g[q], v[q]);
+                        add1(SUM_B, g[q]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) g[q].v[i] = __fmul2_rn(g[q].v[i], w.v[i]);
+                }
                 normalise_back<G>(a.pre, g, v, r, c, per_channel, sum);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) d.v[i] = __fadd2_rn(d.v[i], g.v[i]);
+                for (int q = 0; q < R; ++q)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) d[q].v[i] = __fadd2_rn(d[q].v[i], g[q].v[i]);
             }
             // d = dH
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v.v[i] = __fmul2_rn(d.v[i], both(a.alpha));
-            if (live) put<T, VECD>(dx, v, c);
-            dx += stride;
+            for (int q = 0; q < R; ++q) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[q].v[i] = __fmul2_rn(d[q].v[i], both(a.alpha));
+                if (row + q * GROUPS <= end) put<T, VECD>(dx + q * between, v[q], c);
+            }
+            dx += (long long)R * between;
             if (has_y) {
                 post_weights();
                 if (!KEEP) weights<VECD>(gate_p, 1.f, gate, c);
-                if (live) {
-                    Eight yy = u;
-                    if (POST) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) yy.v[i] = __ffma2_rn(u.v[i], pw.v[i], pb.v[i]);
-                    }
-                    add(SUM_GATE, d, yy);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) d.v[i] = __fmul2_rn(d.v[i], gate.v[i]);
-                if (POST) {
+                for (int q = 0; q < R; ++q) {
+                    const bool live = row + q * GROUPS <= end;
                     if (live) {
-                        add(SUM_POST_W, d, u);
-                        add1(SUM_POST_B, d);
+                        Eight z;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) z.v[i] = yy(q, i);
+                        add(SUM_GATE, d[q], z);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) d.v[i] = __fmul2_rn(d.v[i], pw.v[i]);
-                    normalise_back<G>(a.post, d, u, u_factor, c, per_channel, sum);
+                    for (int i = 0; i < 4; ++i) d[q].v[i] = __fmul2_rn(d[q].v[i], gate.v[i]);
+                    if (POST) {
+                        if (live) {
+                            add(SUM_POST_W, d[q], u[q]);
+                            add1(SUM_POST_B, d[q]);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) d[q].v[i] = __fmul2_rn(d[q].v[i], pw.v[i]);
+                    }
                 }
-                if (live) put<T, VECD>(dy, d, c);
-                dy += stride;
+                if (POST) normalise_back<G>(a.post, d, u, u_factor, c, per_channel, sum);
+#pragma unroll
+                for (int q = 0; q < R; ++q)
+                    if (row + q * GROUPS <= end) put<T, VECD>(dy + q * between, d[q], c);
+                dy += (long long)R * between;
             }
+            if constexpr (STRETCH) in.next();
         }
         if (per_image) {
 #pragma unroll
@@ -603,6 +797,8 @@ __global__ void __launch_bounds__(32 * WARPS) norm_join_kernel(const JoinArgs a)
 struct Plan {
     int group, threads;
     bool wide;
+    int per_sm;             // CTAs of an SM
+    int rows;               // of a group in a round
     int run;                // rows of a CTA
     long long ctas;
 };
@@ -623,16 +819,17 @@ Plan plan(const bra_norm_problem* q, bool backward) {
     const int groups = p.wide ? 1 : p.threads / p.group;
     // as many CTAs as an SM holds at a time, by registers and the ring
     const bool f32 = q->dtype == BRA_F32;
-    int per_sm;
+    int& per_sm = p.per_sm;
     const bool post = q->post != BRA_NORM_NONE;
-    if (p.threads <= 128) per_sm = (backward ? (f32 || post ? 3 : 4) : (f32 || post ? 5 : 6)) * 128 / p.threads;
+    p.rows = backward ? backward_rows(p.threads, post) : q->gate == BRA_GATE_IMAGE || q->per_image ? 1 : forward_rows(p.threads);
+    if (p.threads <= 128) per_sm = (backward ? 3 : p.rows == 2 ? 4 : f32 || post ? 5 : 6) * 128 / p.threads;
     else per_sm = (backward || f32 ? 512 : 1024) / p.threads;
     if (per_sm < 1) per_sm = 1;
     long long most = (long long)kSMs * per_sm;
-    const long long rounds = (rows + groups - 1) / groups;
+    const long long at_once = (long long)groups * p.rows, rounds = (rows + at_once - 1) / at_once;
     if (most > rounds) most = rounds;
     const long long each = (rounds + most - 1) / most;
-    p.run = (int)(each * groups);
+    p.run = (int)(each * at_once);
     p.ctas = (rows + p.run - 1) / p.run;
     return p;
 }
@@ -665,30 +862,50 @@ long long slots_of(const bra_norm_problem* p, const Plan& pl) {
     return pl.ctas + ((p->gate == BRA_GATE_IMAGE || p->per_image) ? p->B : 0);
 }
 
-// Dynamic shared memory of every kernel is a constant times its threads, the most of which THREADS says: allowed once per device.
-template <typename Kernel>
-cudaError_t launch_rows(Kernel kernel, size_t smem, const NormArgs& a, const Plan& pl, cudaStream_t st) {
+template <auto KERNEL>
+cudaError_t launch_rows(size_t smem, const NormArgs& a, const Plan& pl, cudaStream_t st) {
+    static PerDeviceMax attr;
     if (smem > 46 * 1024) {                 // 48 KB less what the kernels have of their own
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t e = attr.ensure((int)smem, [&] { return cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); });
         if (e != cudaSuccess) return e;
     }
-    kernel<<<(unsigned)pl.ctas, pl.threads, smem, st>>>(a);
+    KERNEL<<<(unsigned)pl.ctas, pl.threads, smem, st>>>(a);
     count_launch();
     return cudaGetLastError();
 }
 
+// Slots of rows that are a CTA's: as many as fit beside what the CTA has besides them and the other CTAs of the SM, four at most.
+size_t ring_of(NormArgs& a, const Plan& pl, int esize, int tensors, size_t besides) {
+    a.ring_pitch = (int)(((size_t)pl.rows * a.C * esize + 15) / 16 * 16 + 16);
+    const size_t slot = (size_t)a.ring_pitch * tensors, room = 220 * 1024 / pl.per_sm;
+    const size_t n = room > besides ? (room - besides) / slot : 0;
+    a.ring_slots = (int)(n < NORM_SLOTS ? n : NORM_SLOTS);
+    return slot * a.ring_slots;
+}
+
 template <typename T, bool VECD, int G, int THREADS>
-cudaError_t forward_as(const NormArgs& a, const Plan& pl, cudaStream_t st) {
-    const size_t smem = Ahead<T, VECD, 2, forward_depth(THREADS)>::bytes(pl.threads);
-    return a.post != BRA_NORM_NONE ? launch_rows(norm_forward_kernel<T, VECD, G, true, THREADS>, smem, a, pl, st)
-                                   : launch_rows(norm_forward_kernel<T, VECD, G, false, THREADS>, smem, a, pl, st);
+cudaError_t forward_as(NormArgs a, const Plan& pl, cudaStream_t st) {
+    const bool post = a.post != BRA_NORM_NONE;
+    constexpr int R = forward_rows(THREADS);
+    size_t smem;
+    if (STRETCHES<VECD, G, THREADS>) smem = ring_of(a, pl, sizeof(T), 2, 0);
+    else smem = pl.rows == 1 ? Ahead<T, VECD, 2, forward_depth(THREADS, 1), 1>::bytes(pl.threads) : Ahead<T, VECD, 2, forward_depth(THREADS, R), R>::bytes(pl.threads);
+    if (R == 1 || pl.rows == 1)
+        return post ? launch_rows<norm_forward_kernel<T, VECD, G, true, THREADS, 1>>(smem, a, pl, st)
+                    : launch_rows<norm_forward_kernel<T, VECD, G, false, THREADS, 1>>(smem, a, pl, st);
+    return post ? launch_rows<norm_forward_kernel<T, VECD, G, true, THREADS, R>>(smem, a, pl, st)
+                : launch_rows<norm_forward_kernel<T, VECD, G, false, THREADS, R>>(smem, a, pl, st);
 }
 template <typename T, bool VECD, int G, int THREADS>
-cudaError_t backward_as(const NormArgs& a, const Plan& pl, cudaStream_t st) {
+cudaError_t backward_as(NormArgs a, const Plan& pl, cudaStream_t st) {
     constexpr bool KEEP = THREADS == 128;
-    const size_t smem = sizeof(float) * NORM_E * pl.threads * (KEEP ? (G ? 1 : 0) : SUMS) + Ahead<T, VECD, 4, backward_depth(THREADS)>::bytes(pl.threads);
-    return a.post != BRA_NORM_NONE ? launch_rows(norm_backward_kernel<T, VECD, G, true, THREADS>, smem, a, pl, st)
-                                   : launch_rows(norm_backward_kernel<T, VECD, G, false, THREADS>, smem, a, pl, st);
+    const size_t sums = sizeof(float) * NORM_E * pl.threads * (KEEP ? (G ? 1 : 0) : SUMS);
+    const bool post = a.post != BRA_NORM_NONE;
+    constexpr int RP = backward_rows(THREADS, true), RN = backward_rows(THREADS, false);
+    const size_t smem = sums + (STRETCHES<VECD, G, THREADS> ? ring_of(a, pl, sizeof(T), 4, sums) : post ? Ahead<T, VECD, 4, backward_depth(THREADS, RP), RP>::bytes(pl.threads)
+                                                                                   : Ahead<T, VECD, 4, backward_depth(THREADS, RN), RN>::bytes(pl.threads));
+    return post ? launch_rows<norm_backward_kernel<T, VECD, G, true, THREADS, RP>>(smem, a, pl, st)
+                : launch_rows<norm_backward_kernel<T, VECD, G, false, THREADS, RN>>(smem, a, pl, st);
 }
 template <typename T, bool VECD>
 cudaError_t launch(bool backward, const NormArgs& a, const Plan& pl, cudaStream_t st) {
