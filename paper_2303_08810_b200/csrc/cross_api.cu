@@ -73,8 +73,8 @@ CrossWs cross_ws(const CrossDims& d) {
     L.done = off;  off += align256(sizeof(int32_t) * CROSS_COUNTERS);
     const size_t padded = sizeof(float2) * (size_t)d.B * d.kv * ((d.rows + 63) / 64 * 64), tc = cross_backward_tc_pays(d) ? cross_backward_tc_stats(d) : 0;
     L.stats = off; off += align256(padded > tc ? padded : tc);
-    const size_t f = d.esize != 2 ? cross_attend_simt_part(d) : cross_attend_tc_pays(d) ? cross_attend_tc_part(d) : cross_attend_mma_part(d);
-    const size_t b = d.esize != 2 ? cross_backward_simt_part(d) : cross_backward_tc_pays(d) ? cross_backward_tc_part(d) : cross_backward_mma_part(d);
+    const size_t f = d.esize != 2 ? cross_attend_tf32_part(d) : cross_attend_tc_pays(d) ? cross_attend_tc_part(d) : cross_attend_mma_part(d);
+    const size_t b = d.esize != 2 ? cross_backward_tf32_part(d) : cross_backward_tc_pays(d) ? cross_backward_tc_part(d) : cross_backward_mma_part(d);
     L.part = off;  off += align256(sizeof(float) * (f > b ? f : b));
     L.total = off;
     return L;
@@ -85,7 +85,10 @@ CrossArgs cross_args(const CrossDims& d, char* ws) {
     CrossArgs a = {};
     a.Nq = d.Nq; a.Nk = d.Nk; a.heads = d.heads; a.kv = d.kv; a.group = d.group; a.rows = d.rows;
     a.q_stride = d.q_stride; a.k_stride = d.k_stride; a.v_stride = d.v_stride; a.o_stride = d.o_stride;
-    a.scale = d.scale; a.scale_log2 = d.scale * 1.4426950408889634f;
+    const double scale_log2 = (double)d.scale * 1.4426950408889634074;
+    a.scale = d.scale;
+    a.scale_log2 = (float)scale_log2;
+    a.scale_log2_lo = (float)(scale_log2 - (double)a.scale_log2);
     a.status = reinterpret_cast<int32_t*>(ws + L.status);
     a.done = reinterpret_cast<int32_t*>(ws + L.done);
     a.stats = reinterpret_cast<float2*>(ws + L.stats);
@@ -121,7 +124,7 @@ bra_status bra_cross_attend(const bra_cross_problem* p, const void* Q, const voi
     CrossArgs a = cross_args(d, static_cast<char*>(ws));
     a.Q = Q; a.K = K; a.V = V; a.Oo = O; a.lse = lse; a.key_len = key_len; a.key_mask = key_mask;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = d.esize != 2 ? launch_cross_attend_simt(d, a, st)
+    const cudaError_t e = d.esize != 2 ? launch_cross_attend_tf32(d, a, st)
                           : cross_attend_tc_pays(d) ? launch_cross_attend_tc(d, a, st) : launch_cross_attend_mma(d, a, st);
     return e == cudaSuccess ? BRA_OK : BRA_ERR_CUDA;
 }
@@ -144,7 +147,7 @@ bra_status bra_cross_backward(const bra_cross_problem* p, const void* Q, const v
     a.Q = Q; a.K = K; a.V = V; a.O = O; a.dO = dO; a.dQ = dQ; a.dK = dK; a.dV = dV;
     a.lse = const_cast<float*>(lse); a.key_len = key_len; a.key_mask = key_mask;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = d.esize != 2 ? launch_cross_backward_simt(d, a, st)
+    const cudaError_t e = d.esize != 2 ? launch_cross_backward_tf32(d, a, st)
                           : cross_backward_tc_pays(d) ? launch_cross_backward_tc(d, a, st) : launch_cross_backward_mma(d, a, st);
     return e == cudaSuccess ? BRA_OK : BRA_ERR_CUDA;
 }

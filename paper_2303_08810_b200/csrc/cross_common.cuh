@@ -35,7 +35,7 @@ struct CrossArgs {
     int32_t* status;                                // error words (bra_device_status)
     int Nq, Nk, heads, kv, group, rows;
     long long q_stride, k_stride, v_stride, o_stride;
-    float scale, scale_log2;
+    float scale, scale_log2, scale_log2_lo;         // scale; scale log2 e, and what its rounding left
     int tiles, splits, split_len;                   // output tiles of a pair; parts of the summed axis and their length
     FastDiv tiles_div, splits_div, kv_div, group_div;
 };
@@ -54,7 +54,7 @@ inline void cross_cut(CrossArgs& a, const CrossSplit& s) {
     a.tiles_div = fast_div(s.tiles); a.splits_div = fast_div(s.splits);
 }
 
-// Launchers (bf16: tensor cores; fp32: CUDA cores).  part_floats: what the scratch of their split sums holds.
+// Launchers (bf16: _mma and _tc; fp32: _tf32).  part_floats: what the scratch of their split sums holds.
 cudaError_t launch_cross_attend_mma(const CrossDims& d, CrossArgs a, cudaStream_t st);
 bool cross_attend_tc_pays(const CrossDims& d);
 cudaError_t launch_cross_attend_tc(const CrossDims& d, CrossArgs a, cudaStream_t st);
@@ -64,12 +64,12 @@ size_t cross_backward_tc_stats(const CrossDims& d);         // bytes of its rows
 size_t cross_backward_tc_part(const CrossDims& d);
 size_t cross_attend_tc_part(const CrossDims& d);
 cudaError_t launch_cross_backward_tc(const CrossDims& d, CrossArgs a, cudaStream_t st);
-cudaError_t launch_cross_attend_simt(const CrossDims& d, CrossArgs a, cudaStream_t st);
-cudaError_t launch_cross_backward_simt(const CrossDims& d, CrossArgs a, cudaStream_t st);
+cudaError_t launch_cross_attend_tf32(const CrossDims& d, CrossArgs a, cudaStream_t st);
+cudaError_t launch_cross_backward_tf32(const CrossDims& d, CrossArgs a, cudaStream_t st);
 size_t cross_attend_mma_part(const CrossDims& d);
 size_t cross_backward_mma_part(const CrossDims& d);
-size_t cross_attend_simt_part(const CrossDims& d);
-size_t cross_backward_simt_part(const CrossDims& d);
+size_t cross_attend_tf32_part(const CrossDims& d);
+size_t cross_backward_tf32_part(const CrossDims& d);
 
 #ifdef __CUDACC__
 // This CTA's place: blockIdx.x = (pair * splits + split) * tiles + tile
