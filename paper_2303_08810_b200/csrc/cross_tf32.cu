@@ -50,10 +50,21 @@ __device__ __forceinline__ void mma_tf32(float* d, uint32_t a0, uint32_t a1, uin
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 struct Frag { Split a[4]; };
-__device__ __forceinline__ void mma_split(float* d, const Frag& a, const Split& b0, const Split& b1) {
-    mma_tf32(d, a.a[0].lo, a.a[1].lo, a.a[2].lo, a.a[3].lo, b0.hi, b1.hi);
-    mma_tf32(d, a.a[0].hi, a.a[1].hi, a.a[2].hi, a.a[3].hi, b0.lo, b1.lo);
-    mma_tf32(d, a.a[0].hi, a.a[1].hi, a.a[2].hi, a.a[3].hi, b0.hi, b1.hi);
+// d += sum over k of a[k] * (b0[k], b1[k]).  The tensor core's own additions cut off what does not fit, always towards zero, so a
+// chain of them drifts (75 into one O: 6e-6).  So a few products go to an accumulator of their own, the small ones first, and only its
+// rounded sum is added to d.
+template <int K>
+__device__ __forceinline__ void mma_split(float* d, const Frag (&a)[K], const Split (&b0)[K], const Split (&b1)[K]) {
+    float t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        mma_tf32(t, a[k].a[0].lo, a[k].a[1].lo, a[k].a[2].lo, a[k].a[3].lo, b0[k].hi, b1[k].hi);
+        mma_tf32(t, a[k].a[0].hi, a[k].a[1].hi, a[k].a[2].hi, a[k].a[3].hi, b0[k].lo, b1[k].lo);
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) mma_tf32(t, a[k].a[0].hi, a[k].a[1].hi, a[k].a[2].hi, a[k].a[3].hi, b0[k].hi, b1[k].hi);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d[i] += t[i];
 }
 
 // the LC neighbouring channels of a lane in group g of rows r and r + 8 (null: zeros)
@@ -96,8 +107,13 @@ __device__ __forceinline__ void scores(float (&s)[N][4], const float (&x)[Shape<
                 const float4 v = ptx::lds_f32x4(at + 4 * q);
                 y[q] = v.x; y[q + 1] = v.y; y[q + 2] = v.z; y[q + 3] = v.w;
             }
+            Split b0[S::LC / 2], b1[S::LC / 2];
 #pragma unroll
-            for (int k = 0; k < S::LC / 2; ++k) mma_split(s[n], a[k], split(y[2 * k]), split(y[2 * k + 1]));
+            for (int k = 0; k < S::LC / 2; ++k) {
+                b0[k] = split(y[2 * k]);
+                b1[k] = split(y[2 * k + 1]);
+            }
+            mma_split(s[n], a, b0, b1);
         }
     }
 }
@@ -105,28 +121,43 @@ __device__ __forceinline__ void scores(float (&s)[N][4], const float (&x)[Shape<
 template <int D, int N>
 __device__ __forceinline__ void gather(float (&acc)[Shape<D>::NG][Shape<D>::NB][4], const float (&p)[N][4], uint32_t tile, int row0, int g4, int t4) {
     using S = Shape<D>;
+    constexpr int TWO = N % 2 ? 1 : 2;                          // blocks of eight walked rows at once
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-        Frag a;
-        a.a[0] = split(p[n][0]);
-        a.a[1] = split(p[n][2]);
-        a.a[2] = split(p[n][1]);
-        a.a[3] = split(p[n][3]);
+    for (int n = 0; n < N; n += TWO) {
+        Frag a[TWO];
+#pragma unroll
+        for (int h = 0; h < TWO; ++h) {
+            a[h].a[0] = split(p[n + h][0]);
+            a[h].a[1] = split(p[n + h][2]);
+            a[h].a[2] = split(p[n + h][1]);
+            a[h].a[3] = split(p[n + h][3]);
+        }
 #pragma unroll
         for (int g = 0; g < S::NG; ++g) {
-            const uint32_t at = tile + (row0 + 8 * n + 2 * t4) * S::LD + (g * S::GW + g4 * S::NB) * 4;
-            float y0[4], y1[4];
-            if constexpr (S::NB == 4) {
-                const float4 u = ptx::lds_f32x4(at), v = ptx::lds_f32x4(at + S::LD);
-                y0[0] = u.x; y0[1] = u.y; y0[2] = u.z; y0[3] = u.w;
-                y1[0] = v.x; y1[1] = v.y; y1[2] = v.z; y1[3] = v.w;
-            } else {
-                const float2 u = ptx::lds_f32x2(at), v = ptx::lds_f32x2(at + S::LD);
-                y0[0] = u.x; y0[1] = u.y;
-                y1[0] = v.x; y1[1] = v.y;
+            float y0[TWO][4], y1[TWO][4];
+#pragma unroll
+            for (int h = 0; h < TWO; ++h) {
+                const uint32_t at = tile + (row0 + 8 * (n + h) + 2 * t4) * S::LD + (g * S::GW + g4 * S::NB) * 4;
+                if constexpr (S::NB == 4) {
+                    const float4 u = ptx::lds_f32x4(at), v = ptx::lds_f32x4(at + S::LD);
+                    y0[h][0] = u.x; y0[h][1] = u.y; y0[h][2] = u.z; y0[h][3] = u.w;
+                    y1[h][0] = v.x; y1[h][1] = v.y; y1[h][2] = v.z; y1[h][3] = v.w;
+                } else {
+                    const float2 u = ptx::lds_f32x2(at), v = ptx::lds_f32x2(at + S::LD);
+                    y0[h][0] = u.x; y0[h][1] = u.y;
+                    y1[h][0] = v.x; y1[h][1] = v.y;
+                }
             }
 #pragma unroll
-            for (int j = 0; j < S::NB; ++j) mma_split(acc[g][j], a, split(y0[j]), split(y1[j]));
+            for (int j = 0; j < S::NB; ++j) {
+                Split b0[TWO], b1[TWO];
+#pragma unroll
+                for (int h = 0; h < TWO; ++h) {
+                    b0[h] = split(y0[h][j]);
+                    b1[h] = split(y1[h][j]);
+                }
+                mma_split(acc[g][j], a, b0, b1);
+            }
         }
     }
 }
