@@ -43,7 +43,9 @@ struct Shape {
     // tensor memory: S of the tiles at 0 and 128, O from 256 on; P behind O where there is room, else over S
     static constexpr bool APART = D <= 64;
     static constexpr int TM_O = 256, O_STEP = APART ? 64 : 128, TM_P = APART ? 384 : 0, P_STEP = APART ? 64 : 128;
-    static constexpr int OFF_K = 2 * TILE, OFF_V = OFF_K + STAGES * TILE, OFF_BAR = OFF_V + STAGES * TILE;
+    // pairs of Q tiles in flight: where there is room, the next one's copy runs beside this one's last blocks
+    static constexpr int QS = D <= 64 ? 2 : 1;
+    static constexpr int OFF_K = QS * 2 * TILE, OFF_V = OFF_K + STAGES * TILE, OFF_OUT = OFF_V + STAGES * TILE, OFF_BAR = OFF_OUT + 8 * ROWS32;
     static constexpr size_t smem = OFF_BAR + 384 + 1024;    // barriers; slack for the alignment the swizzle wants
 };
 
@@ -65,8 +67,8 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint64_t* bar = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR);
-    uint64_t *q_full = bar, *q_empty = bar + 1, *s_ready = bar + 2, *s_free = bar + 4, *p_ready = bar + 6, *pv_done = bar + 8,
-             *k_full = bar + 10, *k_empty = k_full + S::STAGES, *v_full = k_empty + S::STAGES, *v_clean = v_full + S::STAGES,
+    uint64_t *q_full = bar, *q_empty = bar + 2, *s_ready = bar + 4, *s_free = bar + 6, *p_ready = bar + 8, *pv_done = bar + 10,
+             *k_full = bar + 12, *k_empty = k_full + S::STAGES, *v_full = k_empty + S::STAGES, *v_clean = v_full + S::STAGES,
              *v_empty = v_clean + S::STAGES, *turn = v_empty + S::STAGES;      // turn: of the four warps of each tile
     uint32_t* slot = reinterpret_cast<uint32_t*>(turn + 8);
     const uint32_t base = smem_u32(smem);
@@ -74,9 +76,8 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
     const CrossArgs& a = g.a;
 
     if (threadIdx.x == 0) {
-        mbar_init(q_full, 1);
-        mbar_init(q_empty, 2);
         for (int w = 0; w < 2; ++w) {
+            mbar_init(q_full + w, 1); mbar_init(q_empty + w, 2);
             mbar_init(s_ready + w, 1); mbar_init(s_free + w, 128); mbar_init(p_ready + w, 128); mbar_init(pv_done + w, 1);
         }
         for (int s = 0; s < S::STAGES; ++s) {
@@ -251,23 +252,17 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
             }
             const int h = x.kvh * a.group + head;
             __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.Oo) + ((long long)x.b * a.Nq + token) * a.o_stride + (long long)h * D;
+            const RowPointers rows = rows_of_warp(live && ok ? out : nullptr, lane);
 #pragma unroll
             for (int k = 0; k < D; k += 32) {
-                uint32_t o[32];
+                uint32_t o[32], v[16];
                 if (x.blocks) {
                     tmem_ld_32x32b_x32(to + k, o);
                     tmem_ld_wait();
                 }
-                if (live && ok) {
 #pragma unroll
-                    for (int q = 0; q < 32; q += 8) {
-                        uint32_t v[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            v[e] = x.blocks ? pack2_bf16(__uint_as_float(o[q + 2 * e]) * inv, __uint_as_float(o[q + 2 * e + 1]) * inv) : 0u;
-                        *reinterpret_cast<uint4*>(out + k + q) = make_uint4(v[0], v[1], v[2], v[3]);
-                    }
-                }
+                for (int e = 0; e < 16; ++e) v[e] = x.blocks ? pack2_bf16(__uint_as_float(o[2 * e]) * inv, __uint_as_float(o[2 * e + 1]) * inv) : 0u;
+                store_rows32(base + S::OFF_OUT + warp * ROWS32, v, rows, k, lane);
             }
             tc_fence_before_sync();
             if (a.lse && live && ok)
@@ -282,15 +277,16 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
             for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
                 const Tile x = tile_of(t);
                 if (!x.blocks) continue;
-                if (n_q) ok = mbar_wait(q_empty, (n_q - 1) & 1, POLL_LIMIT) && ok;
+                const int qb = n_q % S::QS;
+                if (n_q >= S::QS) ok = mbar_wait(q_empty + qb, (n_q / S::QS - 1) & 1, POLL_LIMIT) && ok;
                 ++n_q;
                 if (!ok) break;
                 const uint32_t q_box = (uint32_t)(g.tokens * a.group * S::ROW);
-                mbar_expect_tx(q_full, q_box * S::BOXES * (1 + x.both));
+                mbar_expect_tx(q_full + qb, q_box * S::BOXES * (1 + x.both));
                 for (int w = 0; w <= x.both; ++w)
 #pragma unroll
                     for (int k = 0; k < S::BOXES; ++k)
-                        tma_load_4d(base + w * S::TILE + k * S::PLANE, &map_q, q_full, k * S::BOX, x.kvh * a.group, x.token0 + w * g.tokens, x.b);
+                        tma_load_4d(base + (2 * qb + w) * S::TILE + k * S::PLANE, &map_q, q_full + qb, k * S::BOX, x.kvh * a.group, x.token0 + w * g.tokens, x.b);
                 for (int j = 0; j < x.blocks && ok; ++j, ++n) {
                     const int s = n % S::STAGES;
                     const uint32_t parity = (n / S::STAGES - 1) & 1;
@@ -320,18 +316,19 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
         const uint64_t q_desc = umma_smem_desc(base + w * S::TILE, 16, 8 * S::ROW, S::SWIZZLE);
         const uint64_t k_desc = umma_smem_desc(base + S::OFF_K, 16, 8 * S::ROW, S::SWIZZLE);
         const uint64_t v_desc = umma_smem_desc(base + S::OFF_V, S::BOXES > 1 ? S::PLANE : 16, 8 * S::ROW, S::SWIZZLE);
+        uint32_t qb = 0;                            // this pair's buffer
         auto scores = [&] {
             const int stage = nk % S::STAGES;
             wait_for(k_full + stage, (nk / S::STAGES) & 1, ok);
             if (!ok) return;
             tc_fence_after_sync();
             if (!idle) {
-                const uint64_t kd = k_desc + stage * (S::TILE >> 4);
+                const uint64_t kd = k_desc + stage * (S::TILE >> 4), qd = q_desc + qb * (2 * S::TILE >> 4);
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
                     constexpr int PER = S::BOX / 16;
                     const uint32_t at = (uint32_t)(k / PER * S::PLANE + k % PER * 32) >> 4;
-                    umma_ss(tmem + w * 128, q_desc + at, kd + at, IDESC_S, k);
+                    umma_ss(tmem + w * 128, qd + at, kd + at, IDESC_S, k);
                 }
                 umma_commit(s_ready + w);
             }
@@ -340,14 +337,15 @@ cross_attend_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q
         // stages are given back by both warps
         auto after_scores = [&](const Tile& x, int j) {
             umma_commit(k_empty + (nk - 1) % S::STAGES);
-            if (j + 1 == x.blocks) umma_commit(q_empty);
+            if (j + 1 == x.blocks) umma_commit(q_empty + qb);
         };
         // One lane alone: lanes that only waited along could fall two phases behind a barrier, whose parity then says nothing.
         for (int t = blockIdx.x; lane == 0 && t < g.total && ok; t += gridDim.x) {
             const Tile x = tile_of(t);
             if (!x.blocks) continue;
             idle = w && !x.both;
-            wait_for(q_full, n_q & 1, ok);
+            qb = n_q % S::QS;
+            wait_for(q_full + qb, (n_q / S::QS) & 1, ok);
             ++n_q;
             if (!ok) break;
             scores();

@@ -32,7 +32,9 @@ struct Shape {
     static constexpr int STAGES = D == 128 ? 2 : 4;
     static constexpr uint32_t SWIZZLE = D < 64 ? 4 : 2;
     static constexpr int STAGE = 2 * TILE;                          // Y1, Y2
-    static constexpr int OFF_Y = 2 * TILE, OFF_STAT = OFF_Y + STAGES * STAGE, OFF_BAR = OFF_STAT + (DKV ? STAGES * 1024 : 0);
+    // kept tiles in flight: where there is room, the next one's copy runs beside this one's last blocks (short walks are mostly ends)
+    static constexpr int XS = D <= 64 ? 2 : 1;
+    static constexpr int OFF_Y = XS * 2 * TILE, OFF_STAT = OFF_Y + STAGES * STAGE, OFF_BAR = OFF_STAT + (DKV ? STAGES * 1024 : 0);
     static constexpr size_t smem = OFF_BAR + 256 + 1024;
     // tensor memory: S 0, dP 128, A1 256, A2 behind it, P and dS behind both or over S and dP
     static constexpr bool S_APART = !DKV || D <= 64, DS_APART = !DKV || D <= 64;
@@ -61,8 +63,8 @@ cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, 
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint64_t* bar = reinterpret_cast<uint64_t*>(smem + S::OFF_BAR);
-    uint64_t *x_full = bar, *x_empty = bar + 1, *s_ready = bar + 2, *dp_ready = bar + 3, *s_free = bar + 4, *dp_free = bar + 5, *p_ready = bar + 6,
-             *ds_ready = bar + 7, *pv_done = bar + 8, *acc_done = bar + 9, *y_full = bar + 10, *y_clean = y_full + S::STAGES,
+    uint64_t *x_full = bar, *x_empty = bar + 2, *s_ready = bar + 4, *dp_ready = bar + 5, *s_free = bar + 6, *dp_free = bar + 7, *p_ready = bar + 8,
+             *ds_ready = bar + 9, *pv_done = bar + 10, *acc_done = bar + 11, *y_full = bar + 12, *y_clean = y_full + S::STAGES,
              *y_empty = y_clean + S::STAGES;
     uint32_t* slot = reinterpret_cast<uint32_t*>(y_empty + S::STAGES);
     const uint32_t base = smem_u32(smem);
@@ -70,7 +72,7 @@ cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, 
     const CrossArgs& a = g.a;
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 10; ++i) mbar_init(bar + i, i == 1 ? 2 : i >= 4 && i <= 7 ? 256 : 1);
+        for (int i = 0; i < 12; ++i) mbar_init(bar + i, i == 2 || i == 3 ? 2 : i >= 6 && i <= 9 ? 256 : 1);
         for (int s = 0; s < S::STAGES; ++s) { mbar_init(y_full + s, 1); mbar_init(y_clean + s, 1); mbar_init(y_empty + s, 2); }
         fence_mbar_init();
     }
@@ -315,15 +317,16 @@ cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, 
             for (int t = blockIdx.x; t < g.total && ok; t += gridDim.x) {
                 const Tile x = tile_of(t);
                 if (!x.blocks) continue;
-                if (n_x) ok = mbar_wait(x_empty, (n_x - 1) & 1, POLL_LIMIT) && ok;
+                const int xb = n_x % S::XS;
+                if (n_x >= S::XS) ok = mbar_wait(x_empty + xb, (n_x / S::XS - 1) & 1, POLL_LIMIT) && ok;
                 ++n_x;
                 if (!ok) break;
-                mbar_expect_tx(x_full, 2 * S::BOXES * (DKV ? keys_box : rows_box));
+                mbar_expect_tx(x_full + xb, 2 * S::BOXES * (DKV ? keys_box : rows_box));
 #pragma unroll
                 for (int k = 0; k < S::BOXES; ++k) {
-                    const uint32_t to = base + k * S::PLANE;
-                    tma_load_4d(to, DKV ? &map_k : &map_q, x_full, k * S::BOX, DKV ? x.kvh : x.kvh * a.group, x.x0, x.b);
-                    tma_load_4d(to + S::TILE, DKV ? &map_v : &map_do, x_full, k * S::BOX, DKV ? x.kvh : x.kvh * a.group, x.x0, x.b);
+                    const uint32_t to = base + xb * (2 * S::TILE) + k * S::PLANE;
+                    tma_load_4d(to, DKV ? &map_k : &map_q, x_full + xb, k * S::BOX, DKV ? x.kvh : x.kvh * a.group, x.x0, x.b);
+                    tma_load_4d(to + S::TILE, DKV ? &map_v : &map_do, x_full + xb, k * S::BOX, DKV ? x.kvh : x.kvh * a.group, x.x0, x.b);
                 }
                 for (int j = 0; j < x.blocks && ok; ++j, ++n) {
                     const int s = n % S::STAGES;
@@ -359,27 +362,29 @@ cross_grad_tc_kernel(const TcArgs g, const __grid_constant__ CUtensorMap map_q, 
         static_assert(S::P_HALF == HALF && S::DS_HALF == HALF, "halves of P and dS");
         const bool gathers = DKV || which;
         uint32_t n_x = 0, n = 0;                    // tiles with a walk, blocks so far
+        uint32_t xb = 0;                            // this tile's buffer
         auto scores = [&](uint32_t i, bool last) {
             const uint32_t s = i % S::STAGES;
             wait_for(y_full + s, (i / S::STAGES) & 1, ok);
             if (!ok) return;
             tc_fence_after_sync();
-            const uint64_t y = y_desc + s * (S::STAGE >> 4);
+            const uint64_t y = y_desc + s * (S::STAGE >> 4), xd = x_desc + xb * (2 * S::TILE >> 4);
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 constexpr int PER = S::BOX / 16;
                 const uint32_t at = (uint32_t)(k / PER * S::PLANE + k % PER * 32) >> 4;
-                umma_ss(tmem + which * S::TM_DP, x_desc + at, y + at, IDESC_S, k);
+                umma_ss(tmem + which * S::TM_DP, xd + at, y + at, IDESC_S, k);
             }
             umma_commit(made);
-            if (last) umma_commit(x_empty);
+            if (last) umma_commit(x_empty + xb);
             if (!gathers) umma_commit(y_empty + s);
         };
         // One lane alone: lanes that only waited along could fall two phases behind a barrier, whose parity then says nothing.
         for (int t = blockIdx.x; lane == 0 && t < g.total && ok; t += gridDim.x) {
             const Tile x = tile_of(t);
             if (!x.blocks) continue;
-            wait_for(x_full, n_x & 1, ok);
+            xb = n_x % S::XS;
+            wait_for(x_full + xb, (n_x / S::XS) & 1, ok);
             ++n_x;
             if (ok) scores(n, x.blocks == 1);
             for (int j = 0; j < x.blocks && ok; ++j, ++n) {

@@ -36,6 +36,34 @@ __device__ __forceinline__ void wait_for(uint64_t* bar, uint32_t parity, bool& o
     if (!mbar_try_wait(bar, parity)) ok = mbar_wait(bar, parity, POLL_LIMIT) && ok;
 }
 
+// 32 channels (as 16 pairs) of a warp's 32 rows, thread = row, to global memory by way of 2 KB of shared memory: four lanes a row, so that
+// a store instruction writes eight rows of 64 bytes instead of 32 of 16 (forward of 16 x 1024 x 1024, 12 heads of 64: 98 -> 95 us; the gradients'
+// kernels have no registers left for it: 504 -> 529 us at 2 x 4096 x 4096, 16 heads of 64).
+// to: the row's first channel; null: not stored.
+constexpr int ROWS32 = 2048;
+struct RowPointers { __nv_bfloat16* at[4]; };
+__device__ __forceinline__ RowPointers rows_of_warp(__nv_bfloat16* mine, int lane) {
+    RowPointers p;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        p.at[k] = reinterpret_cast<__nv_bfloat16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), 8 * k + (lane >> 2)));
+    return p;
+}
+__device__ __forceinline__ void store_rows32(uint32_t stage, const uint32_t (&v)[16], const RowPointers& to, int channel, int lane) {
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        sts_f32x4(stage + lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4), __uint_as_float(v[4 * c]), __uint_as_float(v[4 * c + 1]),
+                  __uint_as_float(v[4 * c + 2]), __uint_as_float(v[4 * c + 3]));
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = 8 * k + (lane >> 2), c = lane & 3;
+        const float4 t = lds_f32x4(stage + r * 64 + ((c ^ ((r >> 1) & 3)) << 4));
+        if (to.at[k]) *reinterpret_cast<float4*>(to.at[k] + channel + 8 * c) = t;
+    }
+}
+
 // Work for fewer CTAs than SMs: every walk of `blocks` blocks is cut in parts, as many as make one part an SM at most.  Joining the parts
 // costs about what three blocks do (8 pairs of tiles, 8 heads of 32, forward, whole / cut, us: 2 blocks 7.7 / 9.5, 4 blocks 11.0 / 10.4,
 // 8 blocks 17.4 / 11.1).
