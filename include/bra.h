@@ -279,7 +279,8 @@ bra_status bra_rope(const bra_rope_problem* p, const void* Q, const void* K, con
  * head h / (heads / kv_heads).  Key j of image b is visible iff j < key_len[b] (where key_len is given;
  * below 0 counts as 0) and key_mask[b, j] != 0 (where key_mask is given).  What stands in hidden keys and
  * values, infinities and NaN included, reaches no output.  A query that sees no key (or whose scores
- * are all -inf) has O = 0, lse = -inf and adds nothing to any gradient.
+ * are all -inf) has O = 0, lse = -inf and adds nothing to any gradient.  Of what is visible, an infinity
+ * makes its scores or sums NaN in fp32 problems, whose operands are split in two for the tensor cores.
  */
 typedef struct bra_cross_problem {
     int32_t B, Nq, Nk;        /* images, queries and keys of each */
@@ -291,7 +292,9 @@ typedef struct bra_cross_problem {
 } bra_cross_problem;
 
 /* Scratch size in bytes of both calls (0 if p is invalid).  Host only.  Like the routed attention's, this scratch has to be
- * zero before its first use and is left ready for the next one; calls that share it must be ordered on one stream. */
+ * zero before its first use and is left ready for the next one; calls that share it must be ordered on one stream, and
+ * bra_device_status reads it (BRA_ERR_TIMEOUT: a wait inside a kernel gave up, the outputs are not complete).  Problems of
+ * different sizes may share the scratch of the one that needs most. */
 size_t bra_cross_workspace_bytes(const bra_cross_problem* p);
 
 /*
@@ -328,7 +331,7 @@ typedef enum bra_gate { BRA_GATE_NONE = 0, BRA_GATE_CHANNEL = 1, BRA_GATE_IMAGE 
  * a token.  Everything between x, y and the outputs is fp32; n is made from h before its rounding.
  */
 typedef struct bra_norm_problem {
-    int32_t B, N, C;          /* images, tokens of each, channels (at most 8192) */
+    int32_t B, N, C;          /* images, tokens of each (at most 2^30 together), channels (at most 8192) */
     int32_t pre, post;        /* bra_norm */
     int32_t gate;             /* bra_gate: no gate, fp32 [C], fp32 [B, C] */
     int32_t per_image;        /* nonzero: w and b are fp32 [B, C] (modulated by a condition), else [C] */

@@ -840,7 +840,7 @@ bra_status check(const bra_norm_problem* p) {
     if (!p) return BRA_ERR_NULL;
     if (p->B <= 0 || p->N <= 0 || p->C <= 0) return BRA_ERR_SHAPE;
     if ((long long)p->B * p->N >= (1ll << 40) / p->C) return BRA_ERR_SHAPE;
-    if ((long long)p->B * p->N > 0x7fffffffll) return BRA_ERR_SHAPE;
+    if ((long long)p->B * p->N > (1ll << 30)) return BRA_ERR_SHAPE;         // rows are counted in 32 bits, those asked for ahead too
     if (p->dtype != BRA_F32 && p->dtype != BRA_BF16) return BRA_ERR_DTYPE;
     if (p->pre < BRA_NORM_NONE || p->pre > BRA_NORM_LAYER || p->post < BRA_NORM_NONE || p->post > BRA_NORM_LAYER) return BRA_ERR_UNSUPPORTED;
     if (p->gate < BRA_GATE_NONE || p->gate > BRA_GATE_IMAGE) return BRA_ERR_UNSUPPORTED;

@@ -151,6 +151,7 @@ def norm(bra, kw=None, back=False, ws=A, ws_bytes=1 << 40, **at):
 @pytest.mark.parametrize("kw,code", [
     (dict(B=0), SHAPE), (dict(N=0), SHAPE), (dict(C=0), SHAPE), (dict(eps=-1.0), SHAPE), (dict(eps=math.nan), SHAPE),
     (dict(B=2 ** 20, N=2 ** 20), SHAPE), (dict(dtype=9), DTYPE), (dict(pre=3), UNSUPPORTED), (dict(post=-1), UNSUPPORTED),
+    (dict(B=1, N=2 ** 30 + 1, C=8), SHAPE), (dict(B=2, N=2 ** 30 - 60, C=8), SHAPE),      # rows asked for ahead pass 32 bits
     (dict(gate=3), UNSUPPORTED), (dict(C=8200), UNSUPPORTED),
 ])
 def test_norm_refuses_bad_problems(bra, kw, code, back):
