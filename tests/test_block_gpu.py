@@ -399,6 +399,33 @@ def test_cross_is_the_same_every_time_and_on_other_streams(bra):
                 assert torch.equal(a, b)
 
 
+def test_cross_problems_share_a_scratch(bra):
+    """Problems of different sizes, types and kernels in turn in the scratch of the one that needs most; two streams with one each."""
+    import torch
+    runs = [cross_problem(bra, c, t, seed=9) for c, t in ((CROSS[12], "bf16"), (CROSS_WIDE[8], "bf16"), (CROSS_WIDE[7], "bf16"), (CROSS[2], "f32"),
+                                                          (CROSS[11], "bf16"), (CROSS_WIDE[5], "bf16"), (CROSS[12], "f32"))]
+
+    def run(i, ws):
+        p, Q, K, V, dO, key_len, key_mask, _ = runs[i]
+        O, lse = bra.bra_cross_attend(p, Q, K, V, key_len, key_mask, ws=ws)
+        return (O, lse) + bra.bra_cross_backward(p, Q, K, V, O, lse, dO, key_len, key_mask, ws=ws)
+
+    want = [run(i, bra.cross_workspace(r[0])) for i, r in enumerate(runs)]
+    most = max(bra.cross_workspace_bytes(r[0]) for r in runs)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ws = [torch.zeros(most, device="cuda", dtype=torch.uint8) for _ in streams]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for i in range(len(runs)):
+        for k, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[k].append(run(len(runs) - 1 - i if k else i, ws[k]))
+    for k, st in enumerate(streams):
+        assert bra.bra_device_status(ws[k], stream=st.cuda_stream) == 0
+        for a, b in zip(want, got[k][::-1] if k else got[k]):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
 def test_cross_gradients_by_differences(bra):
     """d(sum O o dO) along a direction of Q, K and V against central differences of the fp32 forward."""
     import torch
@@ -611,6 +638,24 @@ def test_norm_is_the_same_every_time(bra):
         ws.fill_(255)                                        # the scratch needs no initial value
         again = bra.bra_residual_norm_backward(p, x, y, dh, dn, **w, ws=ws)
         assert set(first) == set(again) and all(torch.equal(first[k], again[k]) for k in first)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("C", [24, 64, 250, 765, 1024, 5001, 8192])
+@pytest.mark.parametrize("onto", ["x", "y"])
+def test_norm_over_its_input(bra, C, dtype, onto):
+    """h in the place of x or y: the same bits, rows read ahead or not, and what lies behind the last row stays."""
+    import torch
+    N = 700
+    full = randn(5, N * C + 64, dtype=dtype), randn(6, N * C + 64, dtype=dtype)
+    gate, w = randn(7, C, dtype="f32"), randn(8, C, dtype="f32")
+    p = bra.make_norm_problem(1, N, C, pre="layer", post="rms", gate="channel", dtype=dtype)
+    x, y = (t[:N * C].view(1, N, C) for t in full)
+    h, n = bra.bra_residual_norm(p, x, y, gate=gate, w=w)
+    tail = [t[N * C:].clone() for t in full]
+    h2, n2 = bra.bra_residual_norm(p, x, y, gate=gate, w=w, h=x if onto == "x" else y)
+    assert torch.equal(h, h2) and torch.equal(n, n2)
+    assert all(torch.equal(t[N * C:], u) for t, u in zip(full, tail))
 
 
 # ---------------------------------------------------------------- together
