@@ -6,8 +6,11 @@
 //
 // What bounds it: HBM, every channel read and written once.  A thread has 16 bytes of a head (half layout: and the 16 that belong to
 // them) of one token, makes the (cos, sin) of its pairs once, in registers, and walks the heads of Q and K with them - of all images,
-// where the positions are those that the problem implies - four loads in flight.  No shared memory, no barrier.  The walk is split
-// where there are too few tokens for the GPU.
+// where the positions are those that the problem implies.  No shared memory, no barrier.  The walk is split where there are too few
+// tokens for the GPU.  In fp32 a thread has four loads in flight; in bf16, whose 16 bytes are twice as many channels, registers for
+// more threads are worth more than for more loads of each: one in flight at 40 (neighbours) or 48 registers (halves), against four at 64 and
+// 108, 64 x 56 x 56 tokens, 2 + 2 heads of 32, us: 21.8 / 25.1 and 21.8 / 32.0; 16 x 1024, 12 + 12 heads of 64 26.8 / 32.4 and 23.9 / 36.9;
+// in fp32 one in flight takes 36.7 / 34.5 there, 65537 tokens, 12 + 4 heads of 128 189 / 162.
 // (Measured, B200, 64 x 56 x 56 tokens, 2 + 2 heads of 32, bf16, both ways / 65537 tokens, 12 + 4 heads of 128, fp32: tables in
 // shared memory, a CTA per 64 or 2 tokens 98 / 213 us, CTAs that walk chunks of tokens 86 / 300 us.)
 #include "bra_internal.h"
@@ -19,7 +22,10 @@ namespace bra {
 namespace {
 
 constexpr int ROPE_THREADS = 256;
-constexpr int ROPE_AHEAD = 4;           // units in flight per thread
+constexpr int ROPE_ROUND = 4;           // units that make a thread's angles worth their while
+template <typename T> constexpr int ROPE_AHEAD = sizeof(T) == 2 ? 1 : 4;        // units in flight per thread
+// CTAs of an SM that registers have to allow
+template <typename T, int VEC, bool HALF> constexpr int ROPE_CTAS = sizeof(T) == 2 && VEC >= 4 ? (HALF ? 5 : 6) : 1;
 
 struct RopeArgs {
     const void *Q, *K;
@@ -95,8 +101,9 @@ struct Unit {
 };
 
 template <typename T, int VEC, bool HALF>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const RopeArgs g) {
+__global__ void __launch_bounds__(ROPE_THREADS, ROPE_CTAS<T, VEC, HALF>) rope_kernel(const RopeArgs g) {
     using U = Unit<T, VEC, HALF>;
+    constexpr int AHEAD = ROPE_AHEAD<T>;
     const long long lane = (long long)blockIdx.x * ROPE_THREADS + threadIdx.x;
     if (lane >= g.lanes) return;
     const long long token = g.lanes <= 0x7fffffffll ? (long long)fdiv((uint32_t)lane, g.units_div) : lane / g.units;
@@ -146,10 +153,10 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const RopeArgs g) {
     int j = blockIdx.y * g.part;
     const int end = min(j + g.part, g.walk);
     int b = (int)fdiv((uint32_t)j, g.heads_div), h = j - b * g.all_heads;
-    for (; j < end; j += ROPE_AHEAD) {
-        U unit[ROPE_AHEAD];
+    for (; j < end; j += AHEAD) {
+        U unit[AHEAD];
 #pragma unroll
-        for (int k = 0; k < ROPE_AHEAD; ++k) {
+        for (int k = 0; k < AHEAD; ++k) {
             unit[k].dst = nullptr;
             if (j + k < end) {
                 const bool of_q = h < g.heads;
@@ -161,7 +168,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const RopeArgs g) {
             }
         }
 #pragma unroll
-        for (int k = 0; k < ROPE_AHEAD; ++k)
+        for (int k = 0; k < AHEAD; ++k)
             if (unit[k].dst) unit[k].finish(cs, turned, whole, half);
     }
 }
@@ -252,19 +259,21 @@ bra_status bra_rope(const bra_rope_problem* p, const void* Q, const void* K, con
     a.heads_div = fast_div(a.all_heads);
     a.width_div = fast_div(p->width > 0 ? p->width : 1);
     // Implied positions are the same in every image, and so are the angles.  Where tokens times units are fewer than the threads the
-    // GPU holds twice, the walk over heads and images is split, down to one round of loads a thread.
+    // GPU holds twice, the walk over heads and images is split - down to one unit a thread, where even so there are too few to half fill it,
+    // else in whole rounds (in single units / rounds, us: 16 x 1 token, 12 + 12 heads of 64 2.6 / 3.9, 4 x 999, 6 + 2 heads of 64, fp32 7.0 / 5.0,
+    // 64 x 28 x 28, 4 + 4 heads of 32 15.5 / 14.2).
     const long long own = positions ? tokens : p->N;
     a.lanes = own * a.units;
     const long long walk = positions ? a.all_heads : (long long)p->B * a.all_heads;
     if (walk > (1 << 30)) return BRA_ERR_SHAPE;
     a.walk = (int)walk;
-    const long long enough = 2048ll * 2 * kSMs;
-    long long parts = (enough + a.lanes - 1) / a.lanes, most = (walk + ROPE_AHEAD - 1) / ROPE_AHEAD;
-    parts = parts < most ? parts : most;
-    parts = parts < 65535 ? parts : 65535;
-    const long long rounds = (most + parts - 1) / parts;
-    a.part = (int)(rounds * ROPE_AHEAD);
-    parts = (walk + a.part - 1) / a.part;
+    const long long held = 2048ll * kSMs, want = (2 * held + a.lanes - 1) / a.lanes;
+    long long part = (walk + want - 1) / want;
+    if (a.lanes * walk >= held / 2) part = (part + ROPE_ROUND - 1) / ROPE_ROUND * ROPE_ROUND;
+    const long long least = (walk + 65534) / 65535;
+    part = part > least ? part : least;
+    a.part = (int)part;
+    const long long parts = (walk + part - 1) / part;
     const long long blocks = (a.lanes + ROPE_THREADS - 1) / ROPE_THREADS;
     if (blocks > 0x7fffffffll) return BRA_ERR_SHAPE;
     const dim3 ctas((unsigned)blocks, (unsigned)parts);
