@@ -38,6 +38,7 @@ struct NormArgs {
     float eps, alpha;
     int ring_slots, ring_pitch;             // of rows that are a CTA's
     int sums;                               // which sums are wanted, SUM_* bits
+    int place[5];                           // where in shared memory each of them is
     long long slots;
 };
 
@@ -66,14 +67,14 @@ __device__ __forceinline__ float dot(const Eight& a, const Eight& b) {
 
 // ---------------------------------------------------------------- a thread's eight channels of a row
 // VECD: neighbours (rows start on 16 bytes, C a multiple of eight).  Else channel j of thread t is t + j * group: neighbours over
-// the threads.
-template <bool VECD>
+// the threads.  FULL: more than 256 threads a row, so that only the last of the eight channels may not exist (C > 8 group - 256).
+template <bool VECD, bool FULL>
 struct Cols {
     int t, group, C;
     bool any;                               // VECD: whether these channels exist, all or none
     __device__ __forceinline__ Cols(int t_, int group_, int C_) : t(t_), group(group_), C(C_), any(t_ * NORM_E < C_) {}
     __device__ __forceinline__ int at(int j) const { return VECD ? t * NORM_E + j : t + j * group; }
-    __device__ __forceinline__ bool has(int j) const { return VECD ? any : at(j) < C; }
+    __device__ __forceinline__ bool has(int j) const { return VECD ? any : (FULL && j < NORM_E - 1) || at(j) < C; }
     // f for channels that exist, 0 for the others
     __device__ __forceinline__ float2 only(float f, int i) const {
         return VECD ? both(any ? f : 0.f) : make_float2(has(2 * i) ? f : 0.f, has(2 * i + 1) ? f : 0.f);
@@ -107,7 +108,8 @@ struct Ahead {
     }
     // fetches R rows of every tensor, `between` elements apart, of which those with a number below `end` exist (first: of the first one,
     // then every `groups`th), and moves on by R of them
-    __device__ __forceinline__ void fetch(int first, int groups, int end, int between, const Cols<VECD>& c) {
+    template <typename Channels>
+    __device__ __forceinline__ void fetch(int first, int groups, int end, int between, const Channels& c) {
 #pragma unroll
         for (int k = 0; k < TENSORS; ++k) {
             if (!row[k]) continue;
@@ -136,7 +138,7 @@ struct Ahead {
         }
     }
     __device__ __forceinline__ void arrived() { if constexpr (RING) ptx::cp_async_wait<DEPTH - 1>(); }
-    __device__ __forceinline__ void read(int tensor, int q, int between, Eight& f, const Cols<VECD>& c) const {
+    __device__ __forceinline__ void read(int tensor, int q, Eight& f) const {
         if constexpr (RING) {
             const uint32_t from = base + get + (tensor * R + q) * CHUNKS * pitch;
             if constexpr (VECD && sizeof(T) == 2) {
@@ -215,7 +217,8 @@ struct Stretch {
             if (!ptx::mbar_try_wait(full + count % slots, (count / slots) & 1)) direct = !ptx::mbar_wait(full + count % slots, (count / slots) & 1) || direct;
         }
     }
-    __device__ __forceinline__ void read(int tensor_at, int q, Eight& f, const Cols<VECD>& c) const {
+    template <typename Channels>
+    __device__ __forceinline__ void read(int tensor_at, int q, Eight& f, const Channels& c) const {
         float v[NORM_E] = {};
         if (direct) {
             const T* from = tensor[tensor_at] + (long long)min(row + q, end - 1) * C;
@@ -262,7 +265,8 @@ struct Stretch {
 
 // Which of the two: stretches where a thread would copy its channels one by one, or has no registers to address them by.  Measured
 // (B200, us, forward + backward, stretches / slots of threads): 8 x 1024 x 768 bf16 52 + 92 / 20 + 36, x 4096 59 + 155 / 46 + 107; 765 bf16 21 + 38 /
-// 21 + 47, 5001 fp32 181 + 470 / 205 + 524, 5000 fp32 154 + 383 / 188 + 378.
+// 21 + 47, 5001 fp32 181 + 470 / 205 + 524, 5000 fp32 154 + 383 / 188 + 378.  Since then, by two CTAs an SM up to 640 threads and fewer checks of
+// what exists: 5001 fp32 130 + 300, 5000 fp32 122 + 318, 4500 bf16 183 + 331 -> 116 + 242.
 template <bool VECD, int G, int THREADS>
 constexpr bool STRETCHES = G == 0 && (!VECD || THREADS > 512);
 // rounds in flight of the slots of threads
@@ -270,8 +274,8 @@ __host__ __device__ constexpr int forward_depth(int threads, int rows) { return 
 __host__ __device__ constexpr int backward_rows(int threads, bool post) { return threads <= 128 && !post ? 2 : 1; }
 __host__ __device__ constexpr int backward_depth(int threads, int rows) { return threads > 128 ? 1 : rows == 1 ? 3 : 2; }
 
-template <typename T, bool VECD>
-__device__ __forceinline__ void put(T* row, const Eight& f, const Cols<VECD>& c) {
+template <typename T, bool VECD, bool FULL>
+__device__ __forceinline__ void put(T* row, const Eight& f, const Cols<VECD, FULL>& c) {
     if constexpr (VECD) {
         const float v[NORM_E] = {f.v[0].x, f.v[0].y, f.v[1].x, f.v[1].y, f.v[2].x, f.v[2].y, f.v[3].x, f.v[3].y};
         if (c.any) store_row<NORM_E>(row + c.at(0), v);
@@ -287,8 +291,8 @@ __device__ __forceinline__ void put(T* row, const Eight& f, const Cols<VECD>& c)
     }
 }
 // a vector of C floats; `none` where it is not given
-template <bool VECD>
-__device__ __forceinline__ void weights(const float* p, float none, Eight& f, const Cols<VECD>& c) {
+template <bool VECD, bool FULL>
+__device__ __forceinline__ void weights(const float* p, float none, Eight& f, const Cols<VECD, FULL>& c) {
     f.fill(none);
     if (!p) return;
     if constexpr (VECD) {
@@ -347,8 +351,8 @@ struct RowSum {
 };
 
 // R rows become their normalised forms; their factors go to r.  Channels that do not exist hold zeros and keep them.
-template <int G, int R, bool VECD>
-__device__ __forceinline__ void normalise(int kind, Eight (&v)[R], float (&r)[R], const Cols<VECD>& c, float eps, float per_channel, RowSum<G>& sum) {
+template <int G, int R, typename Channels>
+__device__ __forceinline__ void normalise(int kind, Eight (&v)[R], float (&r)[R], const Channels& c, float eps, float per_channel, RowSum<G>& sum) {
     float s[R];
     if (kind == BRA_NORM_LAYER) {
 #pragma unroll
@@ -373,8 +377,8 @@ __device__ __forceinline__ void normalise(int kind, Eight (&v)[R], float (&r)[R]
 }
 
 // g becomes the gradient of the rows whose normalised forms hat had the gradients g: r (g - hat mean(g hat) [- mean(g)])
-template <int G, int R, bool VECD>
-__device__ __forceinline__ void normalise_back(int kind, Eight (&g)[R], const Eight (&hat)[R], const float (&r)[R], const Cols<VECD>& c, float per_channel,
+template <int G, int R, typename Channels>
+__device__ __forceinline__ void normalise_back(int kind, Eight (&g)[R], const Eight (&hat)[R], const float (&r)[R], const Channels& c, float per_channel,
                                                RowSum<G>& sum) {
     float m[2 * R];
 #pragma unroll
@@ -394,18 +398,19 @@ __device__ __forceinline__ void normalise_back(int kind, Eight (&g)[R], const Ei
 // ---------------------------------------------------------------- forward
 // A CTA's groups take the rows of its run in turn, R rows a round.  All groups make the same number of rounds (those without a row
 // compute on what the ring holds and store nothing), so that the shuffles and barriers of the sums are met by every thread.
-// THREADS: the most a CTA has.  Above 512 a thread has 64 registers: weights are read where they are used, row by row.
+// THREADS: the most a CTA has.  Above 512 a thread has 64 registers (up to 640, 48, for two CTAs an SM): weights are read where they are used,
+// row by row.
 // R: two rows are two independent chains of exchanges and sums (one: 310 instructions a round of four 64-channel rows, 0.62 of them
 // issued per cycle and scheduler).
 __host__ __device__ constexpr int forward_rows(int threads) { return threads <= 128 ? 2 : 1; }
 template <typename T, bool VECD, int G, bool POST, int THREADS, int R>
-__global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(THREADS, THREADS == 384 || THREADS == 640 ? 2 : 0) norm_forward_kernel(const NormArgs a) {
     constexpr bool KEEP = THREADS <= 512, STRETCH = STRETCHES<VECD, G, THREADS>;
     __shared__ float cross[2][32][SUMS_AT_ONCE];
     extern __shared__ __align__(16) char ring[];
     constexpr int GROUPS = G ? THREADS / (G ? G : 1) : 1;
     const int mine = G ? threadIdx.x / (G ? G : 1) : 0;
-    const Cols<VECD> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
+    const Cols<VECD, !VECD && (THREADS > 384)> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
     RowSum<G> sum{cross};
     const int first = (int)(blockIdx.x * (long long)a.run), end = (int)min((long long)first + a.run, a.rows);
     const float per_channel = 1.f / (float)a.C;
@@ -441,8 +446,8 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormArgs a)
     Eight gate, pw, pb, w, b;
     const float *gate_p = a.gate, *w_p = a.w, *b_p = a.b;
     if (POST && KEEP) {
-        weights<VECD>(a.post_w, 1.f, pw, c);
-        weights<VECD>(a.post_b, 0.f, pb, c);
+        weights(a.post_w, 1.f, pw, c);
+        weights(a.post_b, 0.f, pb, c);
     }
     for (int row = first + mine; row - mine < end; row += R * GROUPS) {
         if (row >= image_end && row < end) {
@@ -451,9 +456,9 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormArgs a)
             w_p = row_of(a.w, a.affine_image ? (long long)image * a.C : 0);
             b_p = row_of(a.b, a.affine_image ? (long long)image * a.C : 0);
             if (KEEP) {
-                weights<VECD>(gate_p, 1.f, gate, c);
-                weights<VECD>(w_p, 1.f, w, c);
-                weights<VECD>(b_p, 0.f, b, c);
+                weights(gate_p, 1.f, gate, c);
+                weights(w_p, 1.f, w, c);
+                weights(b_p, 0.f, b, c);
             }
             image_end = per_image ? (int)min((long long)(image + 1) * a.N, (long long)end) : end;
         }
@@ -463,8 +468,8 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormArgs a)
         if constexpr (!STRETCH) {
 #pragma unroll
             for (int q = 0; q < R; ++q) {
-                in.read(0, q, between, v[q], c);
-                if (has_y) in.read(1, q, between, u[q], c);
+                in.read(0, q, v[q]);
+                if (has_y) in.read(1, q, u[q]);
             }
             in.fetch(ask, GROUPS, end, between, c);
             ask += R * GROUPS;
@@ -484,13 +489,13 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormArgs a)
         if (has_y) {
             if (POST) {
                 normalise<G>(a.post, u, r, c, a.eps, per_channel, sum);
-                if (!KEEP) { weights<VECD>(a.post_w, 1.f, pw, c); weights<VECD>(a.post_b, 0.f, pb, c); }
+                if (!KEEP) { weights(a.post_w, 1.f, pw, c); weights(a.post_b, 0.f, pb, c); }
 #pragma unroll
                 for (int q = 0; q < R; ++q)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) u[q].v[i] = __ffma2_rn(u[q].v[i], pw.v[i], pb.v[i]);
             }
-            if (!KEEP) weights<VECD>(gate_p, 1.f, gate, c);
+            if (!KEEP) weights(gate_p, 1.f, gate, c);
 #pragma unroll
             for (int q = 0; q < R; ++q)
 #pragma unroll
@@ -499,17 +504,17 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormArgs a)
         if (h) {
 #pragma unroll
             for (int q = 0; q < R; ++q)
-                if (row + q * GROUPS < end) put<T, VECD>(h + q * between, v[q], c);
+                if (row + q * GROUPS < end) put(h + q * between, v[q], c);
             h += (long long)R * between;
         }
         if (n) {
             normalise<G>(a.pre, v, r, c, a.eps, per_channel, sum);
-            if (!KEEP) { weights<VECD>(w_p, 1.f, w, c); weights<VECD>(b_p, 0.f, b, c); }
+            if (!KEEP) { weights(w_p, 1.f, w, c); weights(b_p, 0.f, b, c); }
 #pragma unroll
             for (int q = 0; q < R; ++q) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[q].v[i] = __ffma2_rn(v[q].v[i], w.v[i], b.v[i]);
-                if (row + q * GROUPS < end) put<T, VECD>(n + q * between, v[q], c);
+                if (row + q * GROUPS < end) put(n + q * between, v[q], c);
             }
             n += (long long)R * between;
         }
@@ -519,20 +524,22 @@ __global__ void __launch_bounds__(THREADS) norm_forward_kernel(const NormArgs a)
 
 // ---------------------------------------------------------------- backward
 // THREADS 128: the sums over tokens stay in registers, and so do the weights.  More (long rows, whose CTAs would have no registers
-// left): the sums are in shared memory, each word its thread's own, and the weights are read again for every row.
+// left): the sums that are wanted are in shared memory, each word its thread's own, and the weights are read again for every row.
+// (All five sums added to, wanted or not, and CTAs of 128 registers a thread, 8 x 1024 x 1536, rms, bf16 49.7 us, now 39.9; x 2500, layer,
+// fp32 222, now 148.)
 template <typename T, bool VECD, int G, bool POST, int THREADS, int R>
-__global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(THREADS, THREADS == 384 ? 2 : 0) norm_backward_kernel(const NormArgs a) {
     constexpr bool KEEP = THREADS == 128, STRETCH = STRETCHES<VECD, G, THREADS>;
     __shared__ float cross[2][32][SUMS_AT_ONCE];
-    // !KEEP: [SUMS][E][threads]; KEEP and several groups: [E][threads], to join the groups; then the ring of rows
+    // !KEEP: [wanted sums][E][threads]; KEEP and several groups: [E][threads], to join the groups; then the ring of rows
     extern __shared__ __align__(16) float sums_sh[];
     constexpr int GROUPS = G ? THREADS / (G ? G : 1) : 1;
     const int mine = G ? threadIdx.x / (G ? G : 1) : 0;
-    const Cols<VECD> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
+    const Cols<VECD, !VECD && (THREADS > 384)> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
     RowSum<G> sum{cross};
     __shared__ uint64_t full[NORM_SLOTS];
     auto rows_in = [&] {
-        float* ring = sums_sh + NORM_E * blockDim.x * (KEEP ? (G ? 1 : 0) : SUMS);
+        float* ring = sums_sh + NORM_E * blockDim.x * (KEEP ? (G ? 1 : 0) : __popc(a.sums));
         if constexpr (!STRETCH) return Ahead<T, VECD, 4, backward_depth(THREADS, R), R>(ring);
         else return Stretch<T, VECD, 4, R>(a, ptx::smem_u32(ring), full);
     };
@@ -546,16 +553,18 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a
     const float per_channel = 1.f / (float)a.C;
 
     Eight acc[KEEP ? SUMS : 1];
-    auto shared_sum = [&](int s, int i) -> float2& { return reinterpret_cast<float2*>(sums_sh)[(s * 4 + i) * blockDim.x + threadIdx.x]; };
+    auto wants = [&](int s) { return (a.sums >> s) & 1; };
+    auto shared_sum = [&](int s, int i) -> float2& { return reinterpret_cast<float2*>(sums_sh)[(a.place[s] * 4 + i) * blockDim.x + threadIdx.x]; };
     auto clear = [&](int s) {
         if constexpr (KEEP) acc[s].fill(0.f);
-        else {
+        else if (wants(s)) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) shared_sum(s, i) = both(0.f);
         }
     };
     // sum s += a * b
     auto add = [&](int s, const Eight& p, const Eight& q) {
+        if (!KEEP && !wants(s)) return;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (KEEP) acc[s].v[i] = __ffma2_rn(p.v[i], q.v[i], acc[s].v[i]);
@@ -563,6 +572,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a
         }
     };
     auto add1 = [&](int s, const Eight& p) {
+        if (!KEEP && !wants(s)) return;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if constexpr (KEEP) acc[s].v[i] = __fadd2_rn(p.v[i], acc[s].v[i]);
@@ -592,10 +602,9 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a
                 }
             }
         }
-        if (mine == 0) put<float, VECD>(to, t, c);
+        if (mine == 0) put(to, t, c);
         clear(s);
     };
-    auto wants = [&](int s) { return (a.sums >> s) & 1; };
     auto of_image = [&](int s) { return s == SUM_GATE ? a.gate_image : s <= SUM_B ? a.affine_image : 0; };
 #pragma unroll
     for (int s = 0; s < SUMS; ++s) clear(s);
@@ -609,9 +618,9 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a
         const float* gate_p = row_of(a.gate, a.gate_image ? (long long)image * a.C : 0);
         const float* w_p = row_of(a.w, a.affine_image ? (long long)image * a.C : 0);
         if (KEEP) {
-            weights<VECD>(gate_p, 1.f, gate, c);
-            weights<VECD>(w_p, 1.f, w, c);
-            if (POST) { weights<VECD>(a.post_w, 1.f, pw, c); weights<VECD>(a.post_b, 0.f, pb, c); }
+            weights(gate_p, 1.f, gate, c);
+            weights(w_p, 1.f, w, c);
+            if (POST) { weights(a.post_w, 1.f, pw, c); weights(a.post_b, 0.f, pb, c); }
         }
         const long long start = (long long)(begin + mine) * a.C;
         const int between = GROUPS * a.C;
@@ -634,11 +643,11 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a
             if constexpr (!STRETCH) {
 #pragma unroll
                 for (int q = 0; q < R; ++q) {
-                    in.read(0, q, between, v[q], c);
-                    if (has_y) in.read(1, q, between, u[q], c);
-                    if (a.dh) in.read(2, q, between, d[q], c);
+                    in.read(0, q, v[q]);
+                    if (has_y) in.read(1, q, u[q]);
+                    if (a.dh) in.read(2, q, d[q]);
                     else d[q].fill(0.f);
-                    if (has_n) in.read(3, q, between, g[q], c);
+                    if (has_n) in.read(3, q, g[q]);
                 }
                 in.fetch(ask, GROUPS, end + 1, between, c);
                 ask += R * GROUPS;
@@ -655,7 +664,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a
                 if (!POST && !has_n) __syncthreads();          // else the sums' barriers say that all have read
             }
             // !KEEP: the weights, as they are used
-            auto post_weights = [&] { if (!KEEP && POST) { weights<VECD>(a.post_w, 1.f, pw, c); weights<VECD>(a.post_b, 0.f, pb, c); } };
+            auto post_weights = [&] { if (!KEEP && POST) { weights(a.post_w, 1.f, pw, c); weights(a.post_b, 0.f, pb, c); } };
             auto yy = [&](int q, int i) { return POST ? __ffma2_rn(u[q].v[i], pw.v[i], pb.v[i]) : u[q].v[i]; };
 #pragma unroll
             for (int q = 0; q < R; ++q)
@@ -664,7 +673,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a
             if (has_y) {
                 if (POST) normalise<G>(a.post, u, u_factor, c, a.eps, per_channel, sum);
                 post_weights();
-                if (!KEEP) weights<VECD>(gate_p, 1.f, gate, c);
+                if (!KEEP) weights(gate_p, 1.f, gate, c);
 #pragma unroll
                 for (int q = 0; q < R; ++q)
 #pragma unroll
@@ -672,7 +681,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a
             }
             if (has_n) {
                 normalise<G>(a.pre, v, r, c, a.eps, per_channel, sum);
-                if (!KEEP) weights<VECD>(w_p, 1.f, w, c);
+                if (!KEEP) weights(w_p, 1.f, w, c);
 #pragma unroll
                 for (int q = 0; q < R; ++q) {
                     if (row + q * GROUPS <= end) {
@@ -693,12 +702,12 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a
             for (int q = 0; q < R; ++q) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[q].v[i] = __fmul2_rn(d[q].v[i], both(a.alpha));
-                if (row + q * GROUPS <= end) put<T, VECD>(dx + q * between, v[q], c);
+                if (row + q * GROUPS <= end) put(dx + q * between, v[q], c);
             }
             dx += (long long)R * between;
             if (has_y) {
                 post_weights();
-                if (!KEEP) weights<VECD>(gate_p, 1.f, gate, c);
+                if (!KEEP) weights(gate_p, 1.f, gate, c);
 #pragma unroll
                 for (int q = 0; q < R; ++q) {
                     const bool live = row + q * GROUPS <= end;
@@ -722,7 +731,7 @@ __global__ void __launch_bounds__(THREADS) norm_backward_kernel(const NormArgs a
                 if (POST) normalise_back<G>(a.post, d, u, u_factor, c, per_channel, sum);
 #pragma unroll
                 for (int q = 0; q < R; ++q)
-                    if (row + q * GROUPS <= end) put<T, VECD>(dy + q * between, d[q], c);
+                    if (row + q * GROUPS <= end) put(dy + q * between, d[q], c);
                 dy += (long long)R * between;
             }
             if constexpr (STRETCH) in.next();
@@ -823,7 +832,15 @@ Plan plan(const bra_norm_problem* q, bool backward) {
     const bool post = q->post != BRA_NORM_NONE;
     p.rows = backward ? backward_rows(p.threads, post) : q->gate == BRA_GATE_IMAGE || q->per_image ? 1 : forward_rows(p.threads);
     if (p.threads <= 128) per_sm = (backward ? 3 : p.rows == 2 ? 4 : f32 || post ? 5 : 6) * 128 / p.threads;
-    else per_sm = (backward || f32 ? 512 : 1024) / p.threads;
+    else if (p.threads > 512) per_sm = !backward && p.threads <= 640 ? 2 : 1;
+    else if (!backward) per_sm = (post ? 768 : f32 ? 800 : 1024) / p.threads;       // 80 registers; three rounds of fp32; 64 registers
+    else {
+        // 80 registers up to 384 threads (six warps a scheduler), 128 above; the sums that there can be and two rows of four tensors in
+        // shared memory
+        const int sums = (q->pre != BRA_NORM_NONE ? 2 : 0) + (q->gate != BRA_GATE_NONE ? 1 : 0) + (post ? 2 : 0);
+        const int by_smem = 224 * 1024 / (NORM_E * (4 * sums + 8 * (f32 ? 4 : 2))), by_regs = p.threads <= 384 ? 768 : 512;
+        per_sm = (by_smem < by_regs ? by_smem : by_regs) / p.threads;
+    }
     if (per_sm < 1) per_sm = 1;
     long long most = (long long)kSMs * per_sm;
     const long long at_once = (long long)groups * p.rows, rounds = (rows + at_once - 1) / at_once;
@@ -899,7 +916,10 @@ cudaError_t forward_as(NormArgs a, const Plan& pl, cudaStream_t st) {
 template <typename T, bool VECD, int G, int THREADS>
 cudaError_t backward_as(NormArgs a, const Plan& pl, cudaStream_t st) {
     constexpr bool KEEP = THREADS == 128;
-    const size_t sums = sizeof(float) * NORM_E * pl.threads * (KEEP ? (G ? 1 : 0) : SUMS);
+    int wanted = 0;
+    for (int s = 0; s < SUMS; ++s)
+        if ((a.sums >> s) & 1) a.place[s] = wanted++;
+    const size_t sums = sizeof(float) * NORM_E * pl.threads * (KEEP ? (G ? 1 : 0) : wanted);
     const bool post = a.post != BRA_NORM_NONE;
     constexpr int RP = backward_rows(THREADS, true), RN = backward_rows(THREADS, false);
     const size_t smem = sums + (STRETCHES<VECD, G, THREADS> ? ring_of(a, pl, sizeof(T), 4, sums) : post ? Ahead<T, VECD, 4, backward_depth(THREADS, RP), RP>::bytes(pl.threads)
@@ -912,7 +932,9 @@ cudaError_t launch(bool backward, const NormArgs& a, const Plan& pl, cudaStream_
 #define BRA_NORM_AS(G, THREADS) (backward ? backward_as<T, VECD, G, THREADS>(a, pl, st) : forward_as<T, VECD, G, THREADS>(a, pl, st))
     if (!pl.wide) return pl.group == 8 ? BRA_NORM_AS(8, 128) : pl.group == 16 ? BRA_NORM_AS(16, 128) : BRA_NORM_AS(32, 128);
     if (pl.threads <= 128) return BRA_NORM_AS(0, 128);
-    return pl.threads <= 512 ? BRA_NORM_AS(0, 512) : BRA_NORM_AS(0, 1024);
+    // 384: registers of two CTAs; the forward pass without a post-norm has those in any case
+    if (pl.threads <= 512) return pl.threads <= 384 && (backward || a.post != BRA_NORM_NONE) ? BRA_NORM_AS(0, 384) : BRA_NORM_AS(0, 512);
+    return pl.threads <= 640 ? BRA_NORM_AS(0, 640) : BRA_NORM_AS(0, 1024);
 #undef BRA_NORM_AS
 }
 cudaError_t launch(bool backward, const bra_norm_problem* p, const NormArgs& a, const Plan& pl, cudaStream_t st) {
