@@ -68,16 +68,20 @@ __device__ __forceinline__ float dot(const Eight& a, const Eight& b) {
 // ---------------------------------------------------------------- a thread's eight channels of a row
 // VECD: neighbours (rows start on 16 bytes, C a multiple of eight).  Else channel j of thread t is t + j * group: neighbours over
 // the threads.  FULL: more than 256 threads a row, so that only the last of the eight channels may not exist (C > 8 group - 256).
-template <bool VECD, bool FULL>
+// QUADS (fp32 rows that start on 16 bytes): four at 4 t, four at 4 group + 4 t, so that a warp's 16-byte accesses are neighbours and fill sectors
+// (with eight neighbours a thread, 16 x 1024 x 512, rms, forward + gradients 35 + 60 us, now 23 + 40; 4 x 1024 x 4096 77 + 198, now 47 + 127).
+template <bool VECD, bool FULL, bool QUADS>
 struct Cols {
     int t, group, C;
-    bool any;                               // VECD: whether these channels exist, all or none
-    __device__ __forceinline__ Cols(int t_, int group_, int C_) : t(t_), group(group_), C(C_), any(t_ * NORM_E < C_) {}
-    __device__ __forceinline__ int at(int j) const { return VECD ? t * NORM_E + j : t + j * group; }
-    __device__ __forceinline__ bool has(int j) const { return VECD ? any : (FULL && j < NORM_E - 1) || at(j) < C; }
+    bool any, more;                         // VECD: whether the first four channels exist and the other four, all or none
+    __device__ __forceinline__ Cols(int t_, int group_, int C_)
+        : t(t_), group(group_), C(C_), any(t_ * (QUADS ? 4 : NORM_E) < C_), more(QUADS ? (group_ + t_) * 4 < C_ : any) {}
+    __device__ __forceinline__ int at(int j) const { return QUADS ? (j >> 2) * group * 4 + t * 4 + (j & 3) : VECD ? t * NORM_E + j : t + j * group; }
+    __device__ __forceinline__ bool half(int k) const { return k ? more : any; }
+    __device__ __forceinline__ bool has(int j) const { return VECD ? half(j >> 2) : (FULL && j < NORM_E - 1) || at(j) < C; }
     // f for channels that exist, 0 for the others
     __device__ __forceinline__ float2 only(float f, int i) const {
-        return VECD ? both(any ? f : 0.f) : make_float2(has(2 * i) ? f : 0.f, has(2 * i + 1) ? f : 0.f);
+        return VECD ? both(half(i >> 1) ? f : 0.f) : make_float2(has(2 * i) ? f : 0.f, has(2 * i + 1) ? f : 0.f);
     }
 };
 
@@ -121,7 +125,7 @@ struct Ahead {
                         const uint32_t to = base + put + (k * R + q) * CHUNKS * pitch;
 #pragma unroll
                         for (int j = 0; j < CHUNKS; ++j) {
-                            if constexpr (VECD) ptx::cp_async_16(to + j * pitch, c.any ? from + j * (16 / (int)sizeof(T)) : from - c.at(0), c.any ? 16 : 0);
+                            if constexpr (VECD) ptx::cp_async_16(to + j * pitch, c.half(j) ? from + (c.at(4 * j) - c.at(0)) : from - c.at(0), c.half(j) ? 16 : 0);
                             else ptx::cp_async_4(to + j * pitch, c.has(j) ? from + j * c.group : from - c.t, c.has(j) ? 4 : 0);
                         }
                     } else {
@@ -223,7 +227,12 @@ struct Stretch {
         if (direct) {
             const T* from = tensor[tensor_at] + (long long)min(row + q, end - 1) * C;
             if constexpr (VECD) {
-                if (c.any) load_row<NORM_E>(from + c.at(0), v);
+                if constexpr (sizeof(T) == 4) {
+                    if (c.any) load_row<4>(from + c.at(0), v);
+                    if (c.more) load_row<4>(from + c.at(4), v + 4);
+                } else {
+                    if (c.any) load_row<NORM_E>(from + c.at(0), v);
+                }
             } else {
 #pragma unroll
                 for (int j = 0; j < NORM_E; ++j) if (c.has(j)) v[j] = (float)from[c.at(j)];
@@ -236,13 +245,12 @@ struct Stretch {
                 widen({__float_as_uint(t.x), __float_as_uint(t.y), __float_as_uint(t.z), __float_as_uint(t.w)}, f);
                 return;
             } else if constexpr (VECD) {
-                if (c.any) {
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const float4 t = ptx::lds_f32x4(at + 16 * k);
+                for (int k = 0; k < 2; ++k)
+                    if (c.half(k)) {
+                        const float4 t = ptx::lds_f32x4(at + 16 * k * c.group);
                         v[4 * k] = t.x; v[4 * k + 1] = t.y; v[4 * k + 2] = t.z; v[4 * k + 3] = t.w;
                     }
-                }
             } else {
 #pragma unroll
                 for (int j = 0; j < NORM_E; ++j)
@@ -266,19 +274,26 @@ struct Stretch {
 // Which of the two: stretches where a thread would copy its channels one by one, or has no registers to address them by.  Measured
 // (B200, us, forward + backward, stretches / slots of threads): 8 x 1024 x 768 bf16 52 + 92 / 20 + 36, x 4096 59 + 155 / 46 + 107; 765 bf16 21 + 38 /
 // 21 + 47, 5001 fp32 181 + 470 / 205 + 524, 5000 fp32 154 + 383 / 188 + 378.  Since then, by two CTAs an SM up to 640 threads and fewer checks of
-// what exists: 5001 fp32 130 + 300, 5000 fp32 122 + 318, 4500 bf16 183 + 331 -> 116 + 242.
+// what exists: 5001 fp32 130 + 300, 5000 fp32 112 + 285, 4500 bf16 183 + 331 -> 116 + 242.
 template <bool VECD, int G, int THREADS>
 constexpr bool STRETCHES = G == 0 && (!VECD || THREADS > 512);
 // rounds in flight of the slots of threads
 __host__ __device__ constexpr int forward_depth(int threads, int rows) { return rows == 1 ? 3 : 2; }
-__host__ __device__ constexpr int backward_rows(int threads, bool post) { return threads <= 128 && !post ? 2 : 1; }
+// Two rows at once, but not with a post-norm of rows that do not come by 16 bytes, which have no registers for it.  With a post-norm, one / two
+// rows, gradients, us: 64 x 3136 x 64 (two CTAs an SM in the place of three) 47.3 / 45.1, 64 x 784 x 128 27.0 / 25.3, 16 x 1024 x 768 (168 registers) 70 / 55.
+__host__ __device__ constexpr int backward_rows(int threads, bool post, bool vec) { return threads <= 128 && (vec || !post) ? 2 : 1; }
 __host__ __device__ constexpr int backward_depth(int threads, int rows) { return threads > 128 ? 1 : rows == 1 ? 3 : 2; }
 
-template <typename T, bool VECD, bool FULL>
-__device__ __forceinline__ void put(T* row, const Eight& f, const Cols<VECD, FULL>& c) {
+template <typename T, bool VECD, bool FULL, bool QUADS>
+__device__ __forceinline__ void put(T* row, const Eight& f, const Cols<VECD, FULL, QUADS>& c) {
     if constexpr (VECD) {
         const float v[NORM_E] = {f.v[0].x, f.v[0].y, f.v[1].x, f.v[1].y, f.v[2].x, f.v[2].y, f.v[3].x, f.v[3].y};
-        if (c.any) store_row<NORM_E>(row + c.at(0), v);
+        if constexpr (QUADS) {
+            if (c.any) store_row<4>(row + c.at(0), v);
+            if (c.more) store_row<4>(row + c.at(4), v + 4);
+        } else {
+            if (c.any) store_row<NORM_E>(row + c.at(0), v);
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < NORM_E; ++j) {
@@ -291,15 +306,18 @@ __device__ __forceinline__ void put(T* row, const Eight& f, const Cols<VECD, FUL
     }
 }
 // a vector of C floats; `none` where it is not given
-template <bool VECD, bool FULL>
-__device__ __forceinline__ void weights(const float* p, float none, Eight& f, const Cols<VECD, FULL>& c) {
+template <bool VECD, bool FULL, bool QUADS>
+__device__ __forceinline__ void weights(const float* p, float none, Eight& f, const Cols<VECD, FULL, QUADS>& c) {
     f.fill(none);
     if (!p) return;
     if constexpr (VECD) {
-        if (c.any) {
-            const float4 a = __ldg(reinterpret_cast<const float4*>(p + c.at(0))), b = __ldg(reinterpret_cast<const float4*>(p + c.at(0)) + 1);
-            f.v[0] = make_float2(a.x, a.y); f.v[1] = make_float2(a.z, a.w); f.v[2] = make_float2(b.x, b.y); f.v[3] = make_float2(b.z, b.w);
-        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (c.half(k)) {
+                const float4 v = __ldg(reinterpret_cast<const float4*>(p + c.at(4 * k)));
+                f.v[2 * k] = make_float2(v.x, v.y);
+                f.v[2 * k + 1] = make_float2(v.z, v.w);
+            }
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -410,7 +428,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 384 || THREADS == 640 ? 2 
     extern __shared__ __align__(16) char ring[];
     constexpr int GROUPS = G ? THREADS / (G ? G : 1) : 1;
     const int mine = G ? threadIdx.x / (G ? G : 1) : 0;
-    const Cols<VECD, !VECD && (THREADS > 384)> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
+    const Cols<VECD, !VECD && (THREADS > 384), VECD && sizeof(T) == 4> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
     RowSum<G> sum{cross};
     const int first = (int)(blockIdx.x * (long long)a.run), end = (int)min((long long)first + a.run, a.rows);
     const float per_channel = 1.f / (float)a.C;
@@ -528,14 +546,14 @@ __global__ void __launch_bounds__(THREADS, THREADS == 384 || THREADS == 640 ? 2 
 // (All five sums added to, wanted or not, and CTAs of 128 registers a thread, 8 x 1024 x 1536, rms, bf16 49.7 us, now 39.9; x 2500, layer,
 // fp32 222, now 148.)
 template <typename T, bool VECD, int G, bool POST, int THREADS, int R>
-__global__ void __launch_bounds__(THREADS, THREADS == 384 ? 2 : 0) norm_backward_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(THREADS, THREADS == 384 || (THREADS == 128 && POST && R == 2 && (G || sizeof(T) == 4)) ? 2 : THREADS == 128 && POST && R == 2 ? 3 : 0) norm_backward_kernel(const NormArgs a) {
     constexpr bool KEEP = THREADS == 128, STRETCH = STRETCHES<VECD, G, THREADS>;
     __shared__ float cross[2][32][SUMS_AT_ONCE];
     // !KEEP: [wanted sums][E][threads]; KEEP and several groups: [E][threads], to join the groups; then the ring of rows
     extern __shared__ __align__(16) float sums_sh[];
     constexpr int GROUPS = G ? THREADS / (G ? G : 1) : 1;
     const int mine = G ? threadIdx.x / (G ? G : 1) : 0;
-    const Cols<VECD, !VECD && (THREADS > 384)> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
+    const Cols<VECD, !VECD && (THREADS > 384), VECD && sizeof(T) == 4> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
     RowSum<G> sum{cross};
     __shared__ uint64_t full[NORM_SLOTS];
     auto rows_in = [&] {
@@ -826,12 +844,13 @@ Plan plan(const bra_norm_problem* q, bool backward) {
         p.threads = 128;
     }
     const int groups = p.wide ? 1 : p.threads / p.group;
-    // as many CTAs as an SM holds at a time, by registers and the ring
+    // as many CTAs as an SM holds at a time, by registers and the ring (the gradients' two rows of fp32, 98 KB for 128 threads: two, not three,
+    // 16 x 1024 x 512 75 -> 60 us)
     const bool f32 = q->dtype == BRA_F32;
     int& per_sm = p.per_sm;
     const bool post = q->post != BRA_NORM_NONE;
-    p.rows = backward ? backward_rows(p.threads, post) : q->gate == BRA_GATE_IMAGE || q->per_image ? 1 : forward_rows(p.threads);
-    if (p.threads <= 128) per_sm = (backward ? 3 : p.rows == 2 ? 4 : f32 || post ? 5 : 6) * 128 / p.threads;
+    p.rows = backward ? backward_rows(p.threads, post, C % NORM_E == 0) : q->gate == BRA_GATE_IMAGE || q->per_image ? 1 : forward_rows(p.threads);
+    if (p.threads <= 128) per_sm = (backward ? (p.rows == 2 && ((f32 && C % NORM_E == 0) || (post && !p.wide)) ? 2 : 3) : p.rows == 2 ? 4 : f32 || post ? 5 : 6) * 128 / p.threads;
     else if (p.threads > 512) per_sm = !backward && p.threads <= 640 ? 2 : 1;
     else if (!backward) per_sm = (post ? 768 : f32 ? 800 : 1024) / p.threads;       // 80 registers; three rounds of fp32; 64 registers
     else {
@@ -921,7 +940,7 @@ cudaError_t backward_as(NormArgs a, const Plan& pl, cudaStream_t st) {
         if ((a.sums >> s) & 1) a.place[s] = wanted++;
     const size_t sums = sizeof(float) * NORM_E * pl.threads * (KEEP ? (G ? 1 : 0) : wanted);
     const bool post = a.post != BRA_NORM_NONE;
-    constexpr int RP = backward_rows(THREADS, true), RN = backward_rows(THREADS, false);
+    constexpr int RP = backward_rows(THREADS, true, VECD), RN = backward_rows(THREADS, false, VECD);
     const size_t smem = sums + (STRETCHES<VECD, G, THREADS> ? ring_of(a, pl, sizeof(T), 4, sums) : post ? Ahead<T, VECD, 4, backward_depth(THREADS, RP), RP>::bytes(pl.threads)
                                                                                    : Ahead<T, VECD, 4, backward_depth(THREADS, RN), RN>::bytes(pl.threads));
     return post ? launch_rows<norm_backward_kernel<T, VECD, G, true, THREADS, RP>>(smem, a, pl, st)
