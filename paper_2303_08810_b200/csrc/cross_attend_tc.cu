@@ -494,7 +494,7 @@ size_t cross_attend_tc_part(const CrossDims& d) {
 // Measured (B200, us, this kernel / the warp-level one).  One block of keys: 64 x 4096 x 20, 4 heads of 32 100 / 96; up to 64 pairs of tiles
 // (8 x 196 x 128, 8 heads of 32) 6.1 / 4.8; 128 pairs 6.2 / 6.6; 4 x 1024 x 100, 8 heads of 64 8.2 / 10.2.  More blocks: 8 x 196 x 256 7.8 / 6.5,
 // 16 x 196 x 256 8.7 / 9.6, 1 x 100 x 512, 8 heads of 64 9.0 / 16.3, 4 x 100 x 2048 16.3 / 31.5, 1 x 1024 x 2048, 4 heads of 128 24 / 57,
-// 2 x 4133 x 4096, 37 heads of 32 474 / 744, of 64 480 / 1137, of 128 643 / 2055.  At most 64 rows: half of a tile and more is empty, and the
+// 2 x 4133 x 4096, 37 heads of 32 465 / 744, of 64 480 / 1137, of 128 601 / 2055.  At most 64 rows: half of a tile and more is empty, and the
 // warp-level kernel splits the keys over more CTAs (16 rows and less have a form of their own there).
 bool cross_attend_tc_pays(const CrossDims& d) {
     if (d.D < 32 || d.group > 128 || d.esize != 2) return false;
