@@ -588,12 +588,13 @@ size_t cross_backward_tc_part(const CrossDims& d) {
 
 // Measured (B200, us, these kernels / the warp-level ones): 1 x 196 x 100, 8 heads of 32 12.7 / 13.2, 64 images 40 / 43; 16 x 100 x 100, 8 heads
 // of 64 13 / 16; 4 x 64 x 512 14.4 / 19.5; 1 x 4096 x 77, 4 heads of 32 17 / 30; 4 x 1024 x 512, 4 heads of 128 36 / 88; 16 x 1024 x 1024, 12 heads of
-// 64 260 / 621.  At most 64 rows: half of a tile and more is empty.
+// 64 260 / 621.  At most 64 keys, half of a block: heads of 32 64 x 196 x 60 39 / 30, 3 x 12680 x 26, 24 heads on 6 217 / 182, but of 64 2 x 4096 x 60
+// 33 / 50, of 128 3 x 2294 x 30, 18 heads on 9 77 / 122.  At most 64 rows: half of a tile and more is empty.
 bool cross_backward_tc_pays(const CrossDims& d) {
     if (d.D < 32 || d.group > 128 || d.esize != 2) return false;
     const long long pairs = (long long)d.B * d.kv;
     if (pairs * row_blocks(d) > (1 << 24) || pairs * ((d.Nk + 127) / 128) > (1 << 24)) return false;
-    return d.rows > 64;
+    return d.rows > 64 && (d.D > 32 || d.Nk > 64);
 }
 
 cudaError_t launch_cross_backward_tc(const CrossDims& d, CrossArgs a, cudaStream_t st) {

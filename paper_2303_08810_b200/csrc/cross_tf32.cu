@@ -17,7 +17,7 @@
 // a reference that moves shows (scores of +-10 would put 10^-6 into P).
 // What bounds it: issue (0.38 - 0.46 instructions a cycle and scheduler at two to three warps, tensor pipe 41 - 58 %): operands are split by every
 // warp that reads them.  Measured (B200), us, forward + gradients, this / on CUDA cores with kept rows in registers and walked ones as
-// broadcasts: 16 x 784 x 196, 4 heads of 32 48 + 134 / 248, 4 x 1024 x 1024, 4 heads of 64 137 + 363 / 1252.
+// broadcasts: 16 x 784 x 196, 4 heads of 32 48 + 131 / 248, 4 x 1024 x 1024, 4 heads of 64 137 + 363 / 1252.
 #include "cross_common.cuh"
 
 #include <math.h>
@@ -458,6 +458,7 @@ __global__ void __launch_bounds__(THREADS, D == 128 ? 1 : 2) cross_grad_tf32_ker
         lo = v == INFINITY ? 0.f : fmaf(v, E_HI, -hi) + v * E_LO;
         return hi;
     };
+    const bool mine = __any_sync(0xffffffffu, in[0] || in[1]);      // a warp without kept rows only copies
     float ref[2], ref_lo[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) ref[i] = base2(lse[i], ref_lo[i]);
@@ -472,7 +473,7 @@ __global__ void __launch_bounds__(THREADS, D == 128 ? 1 : 2) cross_grad_tf32_ker
         const uint32_t y1 = base + (tile & 1) * STAGE, y2 = y1 + S::TILE, st = y2 + S::TILE;
 #pragma unroll 1
         for (int row0 = 0; row0 < S::BN; row0 += 8 * N) {
-            const uint32_t seen = DKV ? 0xffffffffu : keys.word(tile * (S::BN / 32) + (row0 >> 5));
+            const uint32_t seen = !mine || walk_lo + tile * S::BN + row0 >= walk_hi ? 0u : DKV ? 0xffffffffu : keys.word(tile * (S::BN / 32) + (row0 >> 5));
             if (!seen) continue;
             float s[N][4] = {}, dp[N][4] = {};
             scores<D, N>(s, x1, y1, row0, g4, t4);
