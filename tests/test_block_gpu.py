@@ -565,6 +565,40 @@ def test_norm(bra, case, dtype):
     check_norm(bra, case, dtype)
 
 
+# Rows of a CTA of their own, in each size that such CTAs have; many rows a CTA, images that begin inside its run
+NORM_LONG = [
+    (3, 411, 520, "layer", "rms", "image", True, 1.0),
+    (2, 900, 1304, "layer", "layer", "image", True, 0.7),
+    (3, 401, 1777, "rms", "rms", "channel", False, 1.0),
+    (2, 500, 2504, "layer", "none", "channel", False, 1.0),
+    (2, 301, 3333, "layer", "rms", "image", True, 1.0),
+    (1, 700, 4500, "rms", "layer", "channel", False, 1.0),
+    (2, 333, 5000, "layer", "none", "image", False, 1.0),
+    (1, 500, 7001, "rms", "rms", "channel", False, 1.0),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", NORM_LONG, ids=str)
+def test_norm_long_rows(bra, case, dtype):
+    check_norm(bra, case, dtype)
+
+
+@pytest.mark.parametrize("C", [64, 768, 1304, 1777, 4096, 5001])
+def test_norm_gradients_of_some_weights(bra, C):
+    """A sum that is not wanted leaves the others' bits as they are; weights that are not given are ones and zeros."""
+    import torch
+    x, y, dh, dn, w = norm_inputs((2, 150, C, "layer", "rms", "channel", False, 1.0), "bf16")
+    p = bra.make_norm_problem(2, 150, C, pre="layer", post="rms", gate="channel")
+    w["w"], w["post_w"] = torch.ones_like(w["w"]), torch.ones_like(w["post_w"])
+    full = bra.bra_residual_norm_backward(p, x, y, dh, dn, **w)
+    some = {k: w[k] if k in ("gate", "b") else None for k in w}
+    some["post_b"] = w["post_b"]
+    part = bra.bra_residual_norm_backward(p, x, y, dh, dn, **some)
+    assert set(part) == {"dx", "dy", "dgate", "db", "d_post_b"}
+    assert all(torch.equal(part[k], full[k]) for k in part)
+
+
 def test_norm_without_a_block_or_weights(bra):
     """The first norm of a network: h = alpha x, no y; missing weights are ones and zeros; in place into x."""
     import torch
