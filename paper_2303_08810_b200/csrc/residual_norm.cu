@@ -15,13 +15,11 @@
 // every time.  Run c of the rows meets image b at most once, and walking runs and images together raises c or b by at least one from
 // one meeting to the next, so c + b numbers the meetings.
 #include "bra_internal.h"
+#include "norm_cols.h"
 #include "sm100_ptx.cuh"
 
 namespace bra {
 namespace {
-
-constexpr int NORM_E = 8;                   // channels of a thread
-constexpr int NORM_MAX_C = 8192;
 
 struct NormArgs {
     const void *x, *y, *dh, *dn;
@@ -66,22 +64,12 @@ __device__ __forceinline__ float dot(const Eight& a, const Eight& b) {
 }
 
 // ---------------------------------------------------------------- a thread's eight channels of a row
-// VECD: neighbours (rows start on 16 bytes, C a multiple of eight).  Else channel j of thread t is t + j * group: neighbours over
-// the threads.  FULL: more than 256 threads a row, so that only the last of the eight channels may not exist (C > 8 group - 256).
-// QUADS (fp32 rows that start on 16 bytes): four at 4 t, four at 4 group + 4 t, so that a warp's 16-byte accesses are neighbours and fill sectors
-// (with eight neighbours a thread, 16 x 1024 x 512, rms, forward + gradients 35 + 60 us, now 23 + 40; 4 x 1024 x 4096 77 + 198, now 47 + 127).
 template <bool VECD, bool FULL, bool QUADS>
-struct Cols {
-    int t, group, C;
-    bool any, more;                         // VECD: whether the first four channels exist and the other four, all or none
-    __device__ __forceinline__ Cols(int t_, int group_, int C_)
-        : t(t_), group(group_), C(C_), any(t_ * (QUADS ? 4 : NORM_E) < C_), more(QUADS ? (group_ + t_) * 4 < C_ : any) {}
-    __device__ __forceinline__ int at(int j) const { return QUADS ? (j >> 2) * group * 4 + t * 4 + (j & 3) : VECD ? t * NORM_E + j : t + j * group; }
-    __device__ __forceinline__ bool half(int k) const { return k ? more : any; }
-    __device__ __forceinline__ bool has(int j) const { return VECD ? half(j >> 2) : (FULL && j < NORM_E - 1) || at(j) < C; }
+struct Cols : NormCols<VECD, FULL, QUADS> {
+    using NormCols<VECD, FULL, QUADS>::NormCols;
     // f for channels that exist, 0 for the others
     __device__ __forceinline__ float2 only(float f, int i) const {
-        return VECD ? both(half(i >> 1) ? f : 0.f) : make_float2(has(2 * i) ? f : 0.f, has(2 * i + 1) ? f : 0.f);
+        return VECD ? both(this->half(i >> 1) ? f : 0.f) : make_float2(this->has(2 * i) ? f : 0.f, this->has(2 * i + 1) ? f : 0.f);
     }
 };
 
@@ -421,14 +409,14 @@ __device__ __forceinline__ void normalise_back(int kind, Eight (&g)[R], const Ei
 // R: two rows are two independent chains of exchanges and sums (one: 310 instructions a round of four 64-channel rows, 0.62 of them
 // issued per cycle and scheduler).
 __host__ __device__ constexpr int forward_rows(int threads) { return threads <= 128 ? 2 : 1; }
-template <typename T, bool VECD, int G, bool POST, int THREADS, int R>
+template <typename T, bool VECD, int G, bool POST, int THREADS, int R, bool FULL>
 __global__ void __launch_bounds__(THREADS, THREADS == 384 || THREADS == 640 ? 2 : 0) norm_forward_kernel(const NormArgs a) {
     constexpr bool KEEP = THREADS <= 512, STRETCH = STRETCHES<VECD, G, THREADS>;
     __shared__ float cross[2][32][SUMS_AT_ONCE];
     extern __shared__ __align__(16) char ring[];
     constexpr int GROUPS = G ? THREADS / (G ? G : 1) : 1;
     const int mine = G ? threadIdx.x / (G ? G : 1) : 0;
-    const Cols<VECD, !VECD && (THREADS > 384), VECD && sizeof(T) == 4> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
+    const Cols<VECD, FULL, VECD && sizeof(T) == 4> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
     RowSum<G> sum{cross};
     const int first = (int)(blockIdx.x * (long long)a.run), end = (int)min((long long)first + a.run, a.rows);
     const float per_channel = 1.f / (float)a.C;
@@ -545,7 +533,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 384 || THREADS == 640 ? 2 
 // left): the sums that are wanted are in shared memory, each word its thread's own, and the weights are read again for every row.
 // (All five sums added to, wanted or not, and CTAs of 128 registers a thread, 8 x 1024 x 1536, rms, bf16 49.7 us, now 39.9; x 2500, layer,
 // fp32 222, now 148.)
-template <typename T, bool VECD, int G, bool POST, int THREADS, int R>
+template <typename T, bool VECD, int G, bool POST, int THREADS, int R, bool FULL>
 __global__ void __launch_bounds__(THREADS, THREADS == 384 || (THREADS == 128 && POST && R == 2 && (G || sizeof(T) == 4)) ? 2 : THREADS == 128 && POST && R == 2 ? 3 : 0) norm_backward_kernel(const NormArgs a) {
     constexpr bool KEEP = THREADS == 128, STRETCH = STRETCHES<VECD, G, THREADS>;
     __shared__ float cross[2][32][SUMS_AT_ONCE];
@@ -553,7 +541,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 384 || (THREADS == 128 && 
     extern __shared__ __align__(16) float sums_sh[];
     constexpr int GROUPS = G ? THREADS / (G ? G : 1) : 1;
     const int mine = G ? threadIdx.x / (G ? G : 1) : 0;
-    const Cols<VECD, !VECD && (THREADS > 384), VECD && sizeof(T) == 4> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
+    const Cols<VECD, FULL, VECD && sizeof(T) == 4> c(G ? threadIdx.x % (G ? G : 1) : threadIdx.x, G ? G : blockDim.x, a.C);
     RowSum<G> sum{cross};
     __shared__ uint64_t full[NORM_SLOTS];
     auto rows_in = [&] {
@@ -834,15 +822,9 @@ Plan plan(const bra_norm_problem* q, bool backward) {
     Plan p;
     const long long rows = (long long)q->B * q->N;
     const int C = q->C;
-    const int need = (C + NORM_E - 1) / NORM_E;
-    p.wide = need > 32;
-    if (p.wide) {
-        p.group = (need + 31) / 32 * 32;
-        p.threads = p.group;
-    } else {
-        p.group = need <= 8 ? 8 : need <= 16 ? 16 : 32;
-        p.threads = 128;
-    }
+    p.wide = norm_wide(C);
+    p.group = norm_group(C);
+    p.threads = p.wide ? p.group : 128;
     const int groups = p.wide ? 1 : p.threads / p.group;
     // as many CTAs as an SM holds at a time, by registers and the ring (the gradients' two rows of fp32, 98 KB for 128 threads: two, not three,
     // 16 x 1024 x 512 75 -> 60 us)
@@ -919,20 +901,23 @@ size_t ring_of(NormArgs& a, const Plan& pl, int esize, int tensors, size_t besid
     return slot * a.ring_slots;
 }
 
-template <typename T, bool VECD, int G, int THREADS>
+template <typename T, bool VECD, int G, int THREADS, bool FULL>
 cudaError_t forward_as(NormArgs a, const Plan& pl, cudaStream_t st) {
     const bool post = a.post != BRA_NORM_NONE;
     constexpr int R = forward_rows(THREADS);
     size_t smem;
     if (STRETCHES<VECD, G, THREADS>) smem = ring_of(a, pl, sizeof(T), 2, 0);
     else smem = pl.rows == 1 ? Ahead<T, VECD, 2, forward_depth(THREADS, 1), 1>::bytes(pl.threads) : Ahead<T, VECD, 2, forward_depth(THREADS, R), R>::bytes(pl.threads);
-    if (R == 1 || pl.rows == 1)
-        return post ? launch_rows<norm_forward_kernel<T, VECD, G, true, THREADS, 1>>(smem, a, pl, st)
-                    : launch_rows<norm_forward_kernel<T, VECD, G, false, THREADS, 1>>(smem, a, pl, st);
-    return post ? launch_rows<norm_forward_kernel<T, VECD, G, true, THREADS, R>>(smem, a, pl, st)
-                : launch_rows<norm_forward_kernel<T, VECD, G, false, THREADS, R>>(smem, a, pl, st);
+    // the only rows of fewer than 256 threads in so large a kernel are those without a post-norm
+    if constexpr (!VECD && THREADS > 384 && !FULL) return launch_rows<norm_forward_kernel<T, VECD, G, false, THREADS, R, FULL>>(smem, a, pl, st);
+    else if (R == 1 || pl.rows == 1)
+        return post ? launch_rows<norm_forward_kernel<T, VECD, G, true, THREADS, 1, FULL>>(smem, a, pl, st)
+                    : launch_rows<norm_forward_kernel<T, VECD, G, false, THREADS, 1, FULL>>(smem, a, pl, st);
+    else
+        return post ? launch_rows<norm_forward_kernel<T, VECD, G, true, THREADS, R, FULL>>(smem, a, pl, st)
+                    : launch_rows<norm_forward_kernel<T, VECD, G, false, THREADS, R, FULL>>(smem, a, pl, st);
 }
-template <typename T, bool VECD, int G, int THREADS>
+template <typename T, bool VECD, int G, int THREADS, bool FULL>
 cudaError_t backward_as(NormArgs a, const Plan& pl, cudaStream_t st) {
     constexpr bool KEEP = THREADS == 128;
     int wanted = 0;
@@ -943,17 +928,20 @@ cudaError_t backward_as(NormArgs a, const Plan& pl, cudaStream_t st) {
     constexpr int RP = backward_rows(THREADS, true, VECD), RN = backward_rows(THREADS, false, VECD);
     const size_t smem = sums + (STRETCHES<VECD, G, THREADS> ? ring_of(a, pl, sizeof(T), 4, sums) : post ? Ahead<T, VECD, 4, backward_depth(THREADS, RP), RP>::bytes(pl.threads)
                                                                                    : Ahead<T, VECD, 4, backward_depth(THREADS, RN), RN>::bytes(pl.threads));
-    return post ? launch_rows<norm_backward_kernel<T, VECD, G, true, THREADS, RP>>(smem, a, pl, st)
-                : launch_rows<norm_backward_kernel<T, VECD, G, false, THREADS, RN>>(smem, a, pl, st);
+    return post ? launch_rows<norm_backward_kernel<T, VECD, G, true, THREADS, RP, FULL>>(smem, a, pl, st)
+                : launch_rows<norm_backward_kernel<T, VECD, G, false, THREADS, RN, FULL>>(smem, a, pl, st);
 }
 template <typename T, bool VECD>
 cudaError_t launch(bool backward, const NormArgs& a, const Plan& pl, cudaStream_t st) {
-#define BRA_NORM_AS(G, THREADS) (backward ? backward_as<T, VECD, G, THREADS>(a, pl, st) : forward_as<T, VECD, G, THREADS>(a, pl, st))
-    if (!pl.wide) return pl.group == 8 ? BRA_NORM_AS(8, 128) : pl.group == 16 ? BRA_NORM_AS(16, 128) : BRA_NORM_AS(32, 128);
-    if (pl.threads <= 128) return BRA_NORM_AS(0, 128);
-    // 384: registers of two CTAs; the forward pass without a post-norm has those in any case
-    if (pl.threads <= 512) return pl.threads <= 384 && (backward || a.post != BRA_NORM_NONE) ? BRA_NORM_AS(0, 384) : BRA_NORM_AS(0, 512);
-    return pl.threads <= 640 ? BRA_NORM_AS(0, 640) : BRA_NORM_AS(0, 1024);
+#define BRA_NORM_AS(G, THREADS, FULL) (backward ? backward_as<T, VECD, G, THREADS, FULL>(a, pl, st) : forward_as<T, VECD, G, THREADS, FULL>(a, pl, st))
+    if (!pl.wide) return pl.group == 8 ? BRA_NORM_AS(8, 128, false) : pl.group == 16 ? BRA_NORM_AS(16, 128, false) : BRA_NORM_AS(32, 128, false);
+    const NormKernel k = norm_kernel(pl.group, backward, a.post != BRA_NORM_NONE);
+    if (k.threads == 128) return BRA_NORM_AS(0, 128, false);
+    if (k.threads == 384) return BRA_NORM_AS(0, 384, false);
+    // where channels come by eight nothing depends on FULL
+    if constexpr (!VECD)
+        if (!k.full) return forward_as<T, VECD, 0, 512, false>(a, pl, st);
+    return k.threads == 512 ? BRA_NORM_AS(0, 512, !VECD) : k.threads == 640 ? BRA_NORM_AS(0, 640, !VECD) : BRA_NORM_AS(0, 1024, !VECD);
 #undef BRA_NORM_AS
 }
 cudaError_t launch(bool backward, const bra_norm_problem* p, const NormArgs& a, const Plan& pl, cudaStream_t st) {

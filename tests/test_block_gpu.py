@@ -584,6 +584,43 @@ def test_norm_long_rows(bra, case, dtype):
     check_norm(bra, case, dtype)
 
 
+# Without a post-norm, channels that do not come by eight: in each size of kernel, the first and last widths of a number of warps
+ODD = [257, 513, 1023, 1025, 1027, 1111, 1119, 1279, 1281, 1343, 1535, 1537, 1567, 1791, 1793, 2049, 3333, 4095, 4097, 5001, 7001, 8191]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("C", ODD)
+def test_norm_odd_widths(bra, C, dtype):
+    check_norm(bra, (2, 37, C, "layer", "none", "channel", False, 1.0), dtype)
+    check_norm(bra, (3, 5, C, "rms", "none", "image", True, 0.7), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("gate", ["none", "channel", "image"])
+@pytest.mark.parametrize("C", ODD)
+def test_norm_odd_widths_keep_to_their_rows(bra, C, gate, dtype):
+    """What lies behind inputs and weights (NaN) reaches nothing, what lies behind h and n stays, with rows of many CTAs and of one."""
+    import torch
+    for N in (3, 700):
+        behind = lambda t: torch.cat([t.flatten(), torch.full((256,), math.nan, device="cuda", dtype=t.dtype)])[:t.numel()].view(t.shape)      # noqa: E731
+        B = 2 if N == 3 else 1
+        x, y, _, _, w = norm_inputs((B, N, C, "layer", "none", gate, gate == "image", 1.0), dtype)
+        x, y, w = behind(x), behind(y), {k: None if v is None else behind(v) for k, v in w.items()}
+        p = bra.make_norm_problem(B, N, C, pre="layer", gate=gate, per_image=gate == "image", dtype=dtype)
+        want = bra.bra_residual_norm(p, x, y, **w)
+        guard = [torch.full((x.numel() + 256,), 3.0, device="cuda", dtype=x.dtype) for _ in range(2)]
+        h, n = (g[:x.numel()].view(x.shape) for g in guard)
+        bra.bra_residual_norm(p, x, y, h=h, n=n, **w)
+        assert torch.equal(h, want[0]) and torch.equal(n, want[1])
+        assert all(bool((g[x.numel():] == 3.0).all()) for g in guard)
+        X, Y = x.double(), y.double()
+        g = 1.0 if gate == "none" else w["gate"].double()[:, None] if gate == "image" else w["gate"].double()
+        H = X + g * Y
+        # an fma of two roundings and the output's own
+        within(h, H, half_step(dtype) * H.abs() + 2.0 ** -22 * (X.abs() + (g * Y).abs()), "h")
+        assert bool(torch.isfinite(n).all())
+
+
 @pytest.mark.parametrize("C", [64, 768, 1304, 1777, 4096, 5001])
 def test_norm_gradients_of_some_weights(bra, C):
     """A sum that is not wanted leaves the others' bits as they are; weights that are not given are ones and zeros."""

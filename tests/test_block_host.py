@@ -182,6 +182,58 @@ def test_norm_refuses_bad_pointers(bra):
     assert norm(bra, back=True, ws_bytes=need - 1) == WORKSPACE
 
 
+COLUMNS = r"""
+#include <stdio.h>
+#include <vector>
+#include "norm_cols.h"
+using namespace bra;
+static std::vector<int> seen;
+template <bool VECD, bool FULL, bool QUADS> bool each_once(int C, int group) {
+    seen.assign(C, 0);
+    for (int t = 0; t < group; ++t) {
+        const NormCols<VECD, FULL, QUADS> c(t, group, C);
+        for (int j = 0; j < NORM_E; ++j)
+            if (c.has(j)) {
+                if (c.at(j) < 0 || c.at(j) >= C) return false;
+                ++seen[c.at(j)];
+            }
+    }
+    for (int n : seen) if (n != 1) return false;
+    return true;
+}
+int main() {
+    int bad = 0;
+    for (int C = 1; C <= NORM_MAX_C; ++C)
+        for (int backward = 0; backward < 2; ++backward)
+            for (int post = 0; post < 2; ++post) {
+                const int group = norm_group(C);
+                const NormKernel k = norm_kernel(group, backward, post);
+                const bool wide = norm_wide(C), full = wide && k.full;
+                bool ok = !wide || (group <= k.threads && k.threads <= 1024);
+                if (C % NORM_E == 0) ok = ok && each_once<true, false, false>(C, group) && each_once<true, false, true>(C, group);
+                else ok = ok && (full ? each_once<false, true, false>(C, group) : each_once<false, false, false>(C, group));
+                if (!ok && ++bad <= 5) printf("C %d backward %d post %d threads %d of %d\n", C, backward, post, group, k.threads);
+            }
+    printf("%d", bad);
+    return 0;
+}
+"""
+
+
+def test_norm_threads_have_each_channel_once():
+    """Every width, direction and kernel: the threads of a row have all its channels, each once, and none behind the row."""
+    import os
+    import subprocess
+    import tempfile
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    with tempfile.TemporaryDirectory() as d:
+        src, exe = os.path.join(d, "s.cpp"), os.path.join(d, "s")
+        with open(src, "w") as f:
+            f.write(COLUMNS)
+        subprocess.run(["g++", "-O1", "-std=c++17", "-I", os.path.join(root, "paper_2303_08810_b200", "csrc"), "-o", exe, src], check=True)
+        assert subprocess.run([exe], capture_output=True, text=True, check=True).stdout == "0"
+
+
 def test_problem_structures_match_the_header(bra):
     """Sizes as a C compiler lays the structures out."""
     import os
