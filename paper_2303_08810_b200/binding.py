@@ -3,7 +3,9 @@
 Argument marshalling only.  PyTorch provides device memory and the CUDA
 stream; every step of the path runs inside the library's kernels.  If the
 library has not been built, or there is no CUDA device, calls raise: there is
-no fallback.
+no fallback.  `stream` (a torch stream or a handle; None: the current one) is
+where a call runs, and what it is not given (outputs, ws) is allocated there, as
+inside `with torch.cuda.stream(stream)`.
 """
 from __future__ import annotations
 
@@ -215,6 +217,17 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+def _on(stream):
+    """The context in which torch's current stream is `stream`.  What a call makes itself (outputs, scratch and its zeros) has to belong to
+    the stream that the call runs on: from another stream's pool it could be memory that this one still uses, the zeros could come late,
+    and scratch that is let go at the end of the call could be handed out while the kernels count in it."""
+    torch = _torch()
+    if isinstance(stream, torch.cuda.Stream):
+        return torch.cuda.stream(stream)
+    handle = _stream(stream)                                 # 0 and 1 name the default stream in CUDA's interface
+    return torch.cuda.stream(torch.cuda.ExternalStream(handle) if handle > 1 else torch.cuda.default_stream())
+
+
 def _tdtype(p):
     torch = _torch()
     return torch.bfloat16 if p.dtype == BF16 else torch.float32
@@ -227,6 +240,9 @@ def _check(code, where):
 
 def bra_route(p, Q, K, q_mean=None, k_mean=None, index=None, ws=None, stream=None, want_means=True):
     """bra_route: Q, K -> (q_mean, k_mean, index)."""
+    if stream is not None and (ws is None or index is None or q_mean is None or k_mean is None):
+        with _on(stream):
+            return bra_route(p, Q, K, q_mean, k_mean, index, ws, None, want_means)
     torch = _torch()
     lib = load_library()
     ws = workspace(p, Q.device) if ws is None else ws
@@ -252,6 +268,9 @@ def bra_route_static(p, Q, K, index=None, stream=None):
     only when `index` is None does this wrapper ask torch for one.  Calls on
     one device share the array, so keep them ordered on a stream.
     """
+    if stream is not None and index is None:
+        with _on(stream):
+            return bra_route_static(p, Q, K)
     torch = _torch()
     lib = load_library()
     if index is None:
@@ -264,6 +283,9 @@ def bra_route_static(p, Q, K, index=None, stream=None):
 def bra_attend(p, Q, K, V, index, lce_w=None, lce_b=None, O=None, lse=None, ws=None, stream=None,
                want_lse=True):
     """bra_attend: Q, K, V, index -> (O, lse)."""
+    if stream is not None and (ws is None or O is None or lse is None):
+        with _on(stream):
+            return bra_attend(p, Q, K, V, index, lce_w, lce_b, O, lse, ws, None, want_lse)
     torch = _torch()
     lib = load_library()
     ws = workspace(p, Q.device) if ws is None else ws
@@ -279,6 +301,9 @@ def bra_attend(p, Q, K, V, index, lce_w=None, lce_b=None, O=None, lse=None, ws=N
 def bra_forward(p, Q, K, V, lce_w=None, lce_b=None, O=None, index=None, lse=None, ws=None,
                 stream=None, want_index=True, want_lse=True):
     """bra_forward: Q, K, V -> (O, index, lse)."""
+    if stream is not None and (ws is None or O is None or index is None or lse is None):
+        with _on(stream):
+            return bra_forward(p, Q, K, V, lce_w, lce_b, O, index, lse, ws, None, want_index, want_lse)
     torch = _torch()
     lib = load_library()
     ws = workspace(p, Q.device) if ws is None else ws
@@ -296,6 +321,9 @@ def bra_forward(p, Q, K, V, lce_w=None, lce_b=None, O=None, index=None, lse=None
 def bra_backward(p, Q, K, V, index, lce_w, lse, dO, dQ=None, dK=None, dV=None, d_lce_w=None,
                  d_lce_b=None, ws=None, stream=None, want_bias_grad=False):
     """bra_backward: -> (dQ, dK, dV, d_lce_w, d_lce_b)."""
+    if stream is not None and any(t is None for t in (ws, dQ, dK, dV, d_lce_w, d_lce_b)):
+        with _on(stream):
+            return bra_backward(p, Q, K, V, index, lce_w, lse, dO, dQ, dK, dV, d_lce_w, d_lce_b, ws, None, want_bias_grad)
     torch = _torch()
     lib = load_library()
     ws = workspace(p, Q.device) if ws is None else ws
@@ -420,6 +448,9 @@ def _rope_derived(p):
 
 def bra_rope(p, Q, K, freq, positions=None, Qo=None, Ko=None, inverse=False, stream=None):
     """bra_rope: Q, K -> (Qo, Ko).  Pass Q and K as Qo and Ko to rotate in place; inverse=True is the gradient's rotation."""
+    if stream is not None and (Qo is None or Ko is None):
+        with _on(stream):
+            return bra_rope(p, Q, K, freq, positions, Qo, Ko, inverse)
     torch, dev, where = _torch(), _current_device(), "bra_rope"
     t, q, k, pairs, places = _derived(p, _rope_derived)
     q_at = _rows_at(Q, "Q", where, t, dev, q)
@@ -474,6 +505,9 @@ def _cross_mask(key_len, key_mask, where, torch, B, keys, dev):
 
 def bra_cross_attend(p, Q, K, V, key_len=None, key_mask=None, O=None, lse=None, ws=None, stream=None, want_lse=True):
     """bra_cross_attend: Q, K, V -> (O, lse).  key_len int32 [B], key_mask bool or uint8 [B, Nk]."""
+    if stream is not None and (ws is None or O is None or lse is None):
+        with _on(stream):
+            return bra_cross_attend(p, Q, K, V, key_len, key_mask, O, lse, ws, None, want_lse)
     torch, dev, where = _torch(), _current_device(), "bra_cross_attend"
     t, q, k, v, nq, B, keys, stats, n_stats = _derived(p, _cross_derived)
     q_at, k_at, v_at = _rows_at(Q, "Q", where, t, dev, q), _rows_at(K, "K", where, t, dev, k), _rows_at(V, "V", where, t, dev, v)
@@ -498,6 +532,9 @@ def bra_cross_attend(p, Q, K, V, key_len=None, key_mask=None, O=None, lse=None, 
 
 def bra_cross_backward(p, Q, K, V, O, lse, dO, key_len=None, key_mask=None, dQ=None, dK=None, dV=None, ws=None, stream=None):
     """bra_cross_backward: -> (dQ, dK, dV)."""
+    if stream is not None and (ws is None or dQ is None or dK is None or dV is None):
+        with _on(stream):
+            return bra_cross_backward(p, Q, K, V, O, lse, dO, key_len, key_mask, dQ, dK, dV, ws)
     torch, dev, where = _torch(), _current_device(), "bra_cross_backward"
     t, q, k, v, nq, B, keys, stats, n_stats = _derived(p, _cross_derived)
     ins = (_rows_at(Q, "Q", where, t, dev, q), _rows_at(K, "K", where, t, dev, k), _rows_at(V, "V", where, t, dev, v),
@@ -544,6 +581,9 @@ def _weight(t, name, where, numel, dev):
 
 def bra_residual_norm(p, x, y=None, gate=None, post_w=None, post_b=None, w=None, b=None, h=None, n=None, stream=None, want_h=True):
     """bra_residual_norm: x, y -> (h, n): the residual stream behind the block, and what the next block reads."""
+    if stream is not None and (h is None or n is None):
+        with _on(stream):
+            return bra_residual_norm(p, x, y, gate, post_w, post_b, w, b, h, n, None, want_h)
     torch, dev, where = _torch(), _current_device(), "bra_residual_norm"
     t, size, C, gates, affine, normed = _derived(p, _norm_derived)
     x_at = _at(x, "x", where, t, size, dev)
@@ -570,6 +610,9 @@ def bra_residual_norm(p, x, y=None, gate=None, post_w=None, post_b=None, w=None,
 def bra_residual_norm_backward(p, x, y, dh, dn, gate=None, post_w=None, post_b=None, w=None, b=None, dx=None, dy=None, ws=None,
                                stream=None):
     """bra_residual_norm_backward: -> {"dx", "dy", and of the weights that are given "dgate", "d_post_w", "d_post_b", "dw", "db"}."""
+    if stream is not None:                                   # the weights' gradients are always its own
+        with _on(stream):
+            return bra_residual_norm_backward(p, x, y, dh, dn, gate, post_w, post_b, w, b, dx, dy, ws)
     torch, dev, where = _torch(), _current_device(), "bra_residual_norm_backward"
     t, size, C, gates, affine, _ = _derived(p, _norm_derived)
     ins = (_at(x, "x", where, t, size, dev), None if y is None else _at(y, "y", where, t, size, dev), _weight(gate, "gate", where, gates, dev),

@@ -729,6 +729,54 @@ def test_norm_over_its_input(bra, C, dtype, onto):
     assert all(torch.equal(t[N * C:], u) for t, u in zip(full, tail))
 
 
+# ---------------------------------------------------------------- another stream
+def test_calls_on_a_stream_while_the_current_one_is_busy(bra):
+    """Outputs and scratch that the calls make themselves, on a stream given as an object and as a handle, behind nothing of the current
+    stream: the results are there while that one still sleeps, with sums that are split (counters in scratch) and the routed calls too."""
+    import torch
+    # one token on many keys (parts joined by a counter), tiles on tcgen05 whose walks are split
+    crosses = [cross_problem(bra, (2, 1, 3000, 4, 2, 64, None, False), d) for d in ("bf16", "f32")] + \
+        [cross_problem(bra, (1, 100, 1500, 4, 2, 64, None, False), "bf16")]
+    r, freq = bra.make_rope_problem(2, 50, 4, 32), bra.rope_frequencies(32)
+    nc = (2, 60, 96, "layer", "rms", "image", False, 1.0)
+    x, y, dh, dn, w = norm_inputs(nc, "bf16")
+    n = bra.make_norm_problem(2, 60, 96, pre="layer", post="rms", gate="image")
+    qr = randn(21, 2, 50, 128)
+    m = [randn(30 + i, 2, 16, 16, 64) for i in range(4)]
+    lce = randn(35, 64, 5, 5, dtype="f32")
+    p = bra.make_problem(2, 16, 16, 64, heads=2, S=4, topk=2)
+
+    def all_of(**k):
+        out = []
+        for c, Q, K, V, dO, *_ in crosses:
+            O, lse = bra.bra_cross_attend(c, Q, K, V, **k)
+            out += [O, lse, *bra.bra_cross_backward(c, Q, K, V, O, lse, dO, **k)]
+        out += bra.bra_rope(r, qr, qr, freq, **k)
+        out += bra.bra_residual_norm(n, x, y, **w, **k)
+        out += [v for _, v in sorted(bra.bra_residual_norm_backward(n, x, y, dh, dn, **w, **k).items())]
+        O, index, lse = bra.bra_forward(p, *m[:3], lce, **k)
+        out += [O, index, lse, *[t for t in bra.bra_backward(p, *m[:3], index, lce, lse, m[3], **k) if t is not None]]
+        return out
+
+    want = all_of()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for given in (side, side.cuda_stream):
+        all_of(stream=given)                                 # what a first call loads and sets is done
+        torch.cuda.synchronize()
+        for _ in range(3):
+            slept = torch.cuda.Event()
+            torch.cuda._sleep(600_000_000)                   # 0.3 s
+            slept.record()
+            got = all_of(stream=given)
+            side.synchronize()
+            early = not slept.query()
+            with torch.cuda.stream(side):
+                same = all(torch.equal(a, b) for a, b in zip(want, got))
+            assert same and early and len(want) == len(got)
+            torch.cuda.synchronize()
+
+
 # ---------------------------------------------------------------- together
 def block(bra, t, st):
     """Two branches of a block around projected tensors: positions, routed attention, norm, cross attention, norm; and back."""

@@ -234,6 +234,85 @@ def test_norm_threads_have_each_channel_once():
         assert subprocess.run([exe], capture_output=True, text=True, check=True).stdout == "0"
 
 
+# ---------------------------------------------------------------- streams
+class OnStreams:
+    """torch whose allocations and whose current stream are written down (tensors are the host's)."""
+
+    def __init__(self):
+        import contextlib
+        import types
+        import torch
+        self.real, self.current, self.made = torch, 5, []
+
+        class Stream:
+            def __init__(self, handle):
+                self.cuda_stream = handle
+
+        @contextlib.contextmanager
+        def stream(s):
+            before, self.current = self.current, s.cuda_stream
+            yield
+            self.current = before
+
+        self.cuda = types.SimpleNamespace(Stream=Stream, ExternalStream=Stream, stream=stream, default_stream=lambda: Stream(0))
+
+    def __getattr__(self, name):
+        real = getattr(self.real, name)
+        if name not in ("empty", "zeros", "empty_like"):
+            return real
+
+        def make(*args, **kw):
+            self.made.append((name, self.current))
+            return real(*args, **kw)
+        return make
+
+
+@pytest.mark.parametrize("as_object", [True, False])
+@pytest.mark.parametrize("handle", [0, 0x7000])
+def test_what_a_call_makes_belongs_to_its_stream(bra, monkeypatch, handle, as_object):
+    """Outputs, scratch and its zeros, of every call that is given a stream other than the current one."""
+    import torch
+    from paper_2303_08810_b200 import binding
+
+    fake, ran_on = OnStreams(), []
+
+    class Lib:
+        def __getattr__(self, name):
+            if name.endswith("_bytes"):
+                return lambda *args: 512
+            return lambda *args: (ran_on.append((name, args[-1])), 0)[1]
+
+    monkeypatch.setattr(binding, "_TORCH", fake)
+    monkeypatch.setattr(binding, "_LIB", Lib())
+    monkeypatch.setattr(binding, "_RAW_STREAM", lambda: fake.current)
+    monkeypatch.setattr(binding, "_GET_DEVICE", lambda: -1)
+    stream = fake.cuda.Stream(handle) if as_object else handle
+
+    p = bra.make_problem(1, 8, 8, 64, heads=2, S=2, topk=1, dtype="f32")
+    m = torch.zeros(1, 8, 8, 64)
+    idx = torch.zeros(1, 2, 4, 1, dtype=torch.int32)
+    r = bra.make_rope_problem(1, 64, 2, 32, dtype="f32")
+    c = bra.make_cross_problem(1, 64, 64, 2, 32, dtype="f32")
+    n = bra.make_norm_problem(1, 64, 64, gate="channel", dtype="f32")
+    t, w = torch.zeros(1, 64, 64), torch.ones(64)
+    lse = torch.zeros(1, 2, 64)
+    calls = [
+        lambda **k: bra.bra_route(p, m, m, **k), lambda **k: bra.bra_route_static(p, m, m, **k), lambda **k: bra.bra_attend(p, m, m, m, idx, **k),
+        lambda **k: bra.bra_forward(p, m, m, m, **k), lambda **k: bra.bra_backward(p, m, m, m, idx, w, lse, m, **k),
+        lambda **k: bra.bra_rope(r, t, t, torch.ones(16, dtype=torch.float64), **k),
+        lambda **k: bra.bra_cross_attend(c, t, t, t, **k), lambda **k: bra.bra_cross_backward(c, t, t, t, t, lse, t, **k),
+        lambda **k: bra.bra_residual_norm(n, t, t, gate=w, w=w, **k), lambda **k: bra.bra_residual_norm_backward(n, t, t, t, t, gate=w, w=w, **k),
+    ]
+    for call in calls:
+        for where, given in ((handle, dict(stream=stream)), (5, {})):
+            fake.made.clear()
+            ran_on.clear()
+            call(**given)
+            assert len(ran_on) == 1 and ran_on[0][1] == where
+            assert fake.made and all(at == where for _, at in fake.made), ran_on
+            assert fake.current == 5
+
+
 def test_problem_structures_match_the_header(bra):
     """Sizes as a C compiler lays the structures out."""
     import os
