@@ -10,8 +10,9 @@ inside `with torch.cuda.stream(stream)`.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
-from ctypes import c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import byref, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
 
 _LIB = None
 _TORCH = None            # torch, once it has shown a CUDA device
@@ -347,46 +348,86 @@ def bra_device_status(ws, stream=None) -> int:
 
 # ---------------------------------------------------------------- what stands around the attention of a block
 # These calls take tensors of a program's own making (slices of fused projections, masks, positions), so what a wrong one would
-# make the kernels read is checked here: element type, number of elements, order in memory, device.
+# make the kernels read is checked here: element type, shape, order in memory, device.
 _DTYPES = {"f32": F32, "bf16": BF16, F32: F32, BF16: BF16}
 _GET_DEVICE = None
 
 
-def _current_device():
+def _device_getter():
     global _GET_DEVICE
-    if _GET_DEVICE is None:
-        torch = _torch()
-        _GET_DEVICE = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    return _GET_DEVICE()
+    torch = _torch()
+    _GET_DEVICE = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _GET_DEVICE
 
 
-def _at(t, name, where, dtype, numel, device):
-    """Address of a dense tensor of `numel` elements on the current device."""
-    if t is not None and t.dtype is dtype and t.numel() == numel and t.get_device() == device and t.is_contiguous():
+class _Shape(set):
+    """The axes `of` a dense tensor as the kernels count them, and the shapes seen so far that lay its elements out in that order."""
+
+    def __init__(self, *of):
+        super().__init__((of,))
+        self.of = of
+        self.numel = math.prod(of)
+
+
+def _lays_out(shape, axes):
+    """Whether a dense tensor of `shape` has its elements in the order of `axes`: whole axes may be merged and an axis may be split, but none
+    lies elsewhere ([B, heads, N, D] is not [B, N, heads, D], though it has as many elements)."""
+    edges = [1]
+    for n in axes:
+        edges.append(edges[-1] * n)
+    at = 1
+    for n in shape:
+        if n == 1:
+            continue
+        to = at * n
+        if not (at in edges and to in edges):                # else: within one axis
+            end = min((e for e in edges if e > at), default=0)
+            if not to or to > end or end % to:
+                return False
+        at = to
+    return at == edges[-1]
+
+
+def _at(t, name, where, dtype, shape, device):
+    """Address of a dense tensor of `shape` (a _Shape) on the current device."""
+    if t is not None and t.dtype is dtype and t.shape in shape and t.get_device() == device and t.is_contiguous():
         return t.data_ptr()
-    return _refuse(t, name, where, dtype, numel, device)
+    return _look(t, name, where, dtype, shape, device)
 
 
-def _refuse(t, name, where, dtype, numel, device):
+def _look(t, name, where, dtype, shape, device):
     if t is None:
         raise BraError(1, f"{where}: {name}")
     if t.dtype is not dtype:
         raise BraError(4, f"{where}: {name} is {t.dtype}, not {dtype}")
     if t.get_device() != device:
         raise ValueError(f"{where}: {name} is on {t.device}, the current device is cuda:{device}")
-    if t.numel() != numel:
-        raise BraError(2, f"{where}: {name} has {t.numel()} elements, not {numel}")
-    raise BraError(2, f"{where}: {name} is not contiguous")
+    if t.numel() != shape.numel:
+        raise BraError(2, f"{where}: {name} has {t.numel()} elements, not {shape.numel}")
+    if not t.is_contiguous():
+        raise BraError(2, f"{where}: {name} is not contiguous")
+    if not _lays_out(t.shape, shape.of):
+        raise BraError(2, f"{where}: {name} is {list(t.shape)}, not {list(shape.of)}")
+    shape.add(tuple(t.shape))
+    return t.data_ptr()
+
+
+def _ws_at(ws, where, device):
+    if ws.dtype is _TORCH.uint8 and ws.get_device() == device and ws.is_contiguous():
+        return ws.data_ptr()
+    return _look(ws, "ws", where, _TORCH.uint8, _Shape(ws.numel()), device)
 
 
 def _rows_at(t, name, where, dtype, device, tokens):
-    """Address of a tensor of tokens = (images, tokens, channels, stride, elements): dense, or a [images, tokens, channels] view whose
+    """Address of a tensor of tokens = (images, tokens, channels, stride, shape): dense, or a [images, tokens, channels] view whose
     tokens lie `stride` elements apart."""
-    B, N, C, stride, numel = tokens
+    B, N, C, stride, shape = tokens
     if stride == C:
-        return _at(t, name, where, dtype, numel, device)
-    if t is None or t.dtype is not dtype or t.get_device() != device or t.numel() != numel:
-        return _refuse(t, name, where, dtype, numel, device)
+        if t is not None and t.dtype is dtype and t.shape in shape and t.get_device() == device and t.is_contiguous():      # _at, a call less
+            return t.data_ptr()
+        return _look(t, name, where, dtype, shape, device)
+    if t is None or t.dtype is not dtype or t.get_device() != device:
+        return _look(t, name, where, dtype, shape, device)
     if t.dim() != 3 or tuple(t.shape) != (B, N, C) or (C > 1 and t.stride(2) != 1) or (N > 1 and t.stride(1) != stride) or \
             (B > 1 and t.stride(0) != N * stride):
         raise BraError(2, f"{where}: {name} is not a [{B}, {N}, {C}] view with {stride} elements from token to token")
@@ -398,12 +439,14 @@ _DERIVED = {}
 
 
 def _derived(p, make):
-    key = bytes(p)
-    d = _DERIVED.get((make, key))
-    if d is None:
-        if len(_DERIVED) > 4096:
-            _DERIVED.clear()
-        d = _DERIVED[make, key] = make(p)
+    key = make, bytes(p)
+    try:
+        return _DERIVED[key]
+    except KeyError:
+        pass
+    if len(_DERIVED) > 4096:
+        _DERIVED.clear()
+    d = _DERIVED[key] = make(p)
     return d
 
 
@@ -441,9 +484,10 @@ def rope_frequencies(rot_dim, axes=1, base=10000.0, scaling="none", factor=1.0, 
 
 
 def _rope_derived(p):
-    q, k, n = p.heads * p.head_dim, p.kv_heads * p.head_dim, p.B * p.N
-    return (_tdtype(p), (p.B, p.N, q, p.q_stride or q, n * q), (p.B, p.N, k, p.k_stride or k, n * k),
-            p.rot_dim // p.axes // 2 if p.axes else 0, n * p.axes)
+    q, k = p.heads * p.head_dim, p.kv_heads * p.head_dim
+    return (_tdtype(p), (p.B, p.N, q, p.q_stride or q, _Shape(p.B, p.N, p.heads, p.head_dim)),
+            (p.B, p.N, k, p.k_stride or k, _Shape(p.B, p.N, p.kv_heads, p.head_dim)),
+            _Shape(p.rot_dim // p.axes // 2 if p.axes else 0), _Shape(p.B, p.N, p.axes))
 
 
 def bra_rope(p, Q, K, freq, positions=None, Qo=None, Ko=None, inverse=False, stream=None):
@@ -451,7 +495,7 @@ def bra_rope(p, Q, K, freq, positions=None, Qo=None, Ko=None, inverse=False, str
     if stream is not None and (Qo is None or Ko is None):
         with _on(stream):
             return bra_rope(p, Q, K, freq, positions, Qo, Ko, inverse)
-    torch, dev, where = _torch(), _current_device(), "bra_rope"
+    torch, dev, where = _TORCH or _torch(), (_GET_DEVICE or _device_getter())(), "bra_rope"
     t, q, k, pairs, places = _derived(p, _rope_derived)
     q_at = _rows_at(Q, "Q", where, t, dev, q)
     k_at = _rows_at(K, "K", where, t, dev, k) if k[2] or K is not None else None
@@ -469,7 +513,7 @@ def bra_rope(p, Q, K, freq, positions=None, Qo=None, Ko=None, inverse=False, str
         ko_at = Ko.data_ptr()
     else:
         ko_at = _rows_at(Ko, "Ko", where, t, dev, k)
-    code = (_LIB or load_library()).bra_rope(ctypes.byref(p), q_at, k_at, at, f_at, 1 if inverse else 0, qo_at, ko_at, _stream(stream))
+    code = (_LIB or load_library()).bra_rope(byref(p), q_at, k_at, at, f_at, 1 if inverse else 0, qo_at, ko_at, _stream(stream))
     if code:
         raise BraError(code, where)
     return Qo, Ko
@@ -492,13 +536,13 @@ def cross_workspace(p: BraCrossProblem, device="cuda"):
 
 def _cross_derived(p):
     C, Ck = p.heads * p.head_dim, p.kv_heads * p.head_dim
-    nq, nk = p.B * p.Nq * C, p.B * p.Nk * Ck
-    return (_tdtype(p), (p.B, p.Nq, C, p.q_stride or C, nq), (p.B, p.Nk, Ck, p.k_stride or Ck, nk), (p.B, p.Nk, Ck, p.v_stride or Ck, nk),
-            nq, p.B, p.B * p.Nk, (p.B, p.heads, p.Nq), p.B * p.heads * p.Nq)
+    q, k = _Shape(p.B, p.Nq, p.heads, p.head_dim), _Shape(p.B, p.Nk, p.kv_heads, p.head_dim)
+    return (_tdtype(p), (p.B, p.Nq, C, p.q_stride or C, q), (p.B, p.Nk, Ck, p.k_stride or Ck, k), (p.B, p.Nk, Ck, p.v_stride or Ck, k),
+            q, _Shape(p.B), _Shape(p.B, p.Nk), _Shape(p.B, p.heads, p.Nq))
 
 
-def _cross_mask(key_len, key_mask, where, torch, B, keys, dev):
-    return (None if key_len is None else _at(key_len, "key_len", where, torch.int32, B, dev),
+def _cross_mask(key_len, key_mask, where, torch, images, keys, dev):
+    return (None if key_len is None else _at(key_len, "key_len", where, torch.int32, images, dev),
             None if key_mask is None else
             _at(key_mask, "key_mask", where, torch.bool if key_mask.dtype is torch.bool else torch.uint8, keys, dev))
 
@@ -508,23 +552,23 @@ def bra_cross_attend(p, Q, K, V, key_len=None, key_mask=None, O=None, lse=None, 
     if stream is not None and (ws is None or O is None or lse is None):
         with _on(stream):
             return bra_cross_attend(p, Q, K, V, key_len, key_mask, O, lse, ws, None, want_lse)
-    torch, dev, where = _torch(), _current_device(), "bra_cross_attend"
-    t, q, k, v, nq, B, keys, stats, n_stats = _derived(p, _cross_derived)
+    torch, dev, where = _TORCH or _torch(), (_GET_DEVICE or _device_getter())(), "bra_cross_attend"
+    t, q, k, v, dense, images, keys, stats = _derived(p, _cross_derived)
     q_at, k_at, v_at = _rows_at(Q, "Q", where, t, dev, q), _rows_at(K, "K", where, t, dev, k), _rows_at(V, "V", where, t, dev, v)
-    len_at, mask_at = _cross_mask(key_len, key_mask, where, torch, B, keys, dev)
+    len_at, mask_at = _cross_mask(key_len, key_mask, where, torch, images, keys, dev)
     if ws is None:
         ws = cross_workspace(p, Q.device)
     if O is None:
         O = torch.empty(Q.shape, dtype=t, device=Q.device)
         o_at = O.data_ptr()
     else:
-        o_at = _at(O, "O", where, t, nq, dev)
+        o_at = _at(O, "O", where, t, dense, dev)
     if lse is None and want_lse:
-        lse = torch.empty(stats, dtype=torch.float32, device=Q.device)
+        lse = torch.empty(stats.of, dtype=torch.float32, device=Q.device)
     n_ws = ws.numel()
     code = (_LIB or load_library()).bra_cross_attend(
-        ctypes.byref(p), q_at, k_at, v_at, len_at, mask_at, o_at, None if lse is None else _at(lse, "lse", where, torch.float32, n_stats, dev),
-        _at(ws, "ws", where, torch.uint8, n_ws, dev), n_ws, _stream(stream))
+        byref(p), q_at, k_at, v_at, len_at, mask_at, o_at, None if lse is None else _at(lse, "lse", where, torch.float32, stats, dev),
+        _ws_at(ws, where, dev), n_ws, _stream(stream))
     if code:
         raise BraError(code, where)
     return O, lse
@@ -535,11 +579,11 @@ def bra_cross_backward(p, Q, K, V, O, lse, dO, key_len=None, key_mask=None, dQ=N
     if stream is not None and (ws is None or dQ is None or dK is None or dV is None):
         with _on(stream):
             return bra_cross_backward(p, Q, K, V, O, lse, dO, key_len, key_mask, dQ, dK, dV, ws)
-    torch, dev, where = _torch(), _current_device(), "bra_cross_backward"
-    t, q, k, v, nq, B, keys, stats, n_stats = _derived(p, _cross_derived)
+    torch, dev, where = _TORCH or _torch(), (_GET_DEVICE or _device_getter())(), "bra_cross_backward"
+    t, q, k, v, dense, images, keys, stats = _derived(p, _cross_derived)
     ins = (_rows_at(Q, "Q", where, t, dev, q), _rows_at(K, "K", where, t, dev, k), _rows_at(V, "V", where, t, dev, v),
-           *_cross_mask(key_len, key_mask, where, torch, B, keys, dev), _at(O, "O", where, t, nq, dev),
-           _at(lse, "lse", where, torch.float32, n_stats, dev), _at(dO, "dO", where, t, nq, dev))
+           *_cross_mask(key_len, key_mask, where, torch, images, keys, dev), _at(O, "O", where, t, dense, dev),
+           _at(lse, "lse", where, torch.float32, stats, dev), _at(dO, "dO", where, t, dense, dev))
     if ws is None:
         ws = cross_workspace(p, Q.device)
     dQ = _like(Q, q) if dQ is None else dQ
@@ -547,8 +591,8 @@ def bra_cross_backward(p, Q, K, V, O, lse, dO, key_len=None, key_mask=None, dQ=N
     dV = _like(V, v) if dV is None else dV
     n_ws = ws.numel()
     code = (_LIB or load_library()).bra_cross_backward(
-        ctypes.byref(p), *ins, _rows_at(dQ, "dQ", where, t, dev, q), _rows_at(dK, "dK", where, t, dev, k), _rows_at(dV, "dV", where, t, dev, v),
-        _at(ws, "ws", where, torch.uint8, n_ws, dev), n_ws, _stream(stream))
+        byref(p), *ins, _rows_at(dQ, "dQ", where, t, dev, q), _rows_at(dK, "dK", where, t, dev, k), _rows_at(dV, "dV", where, t, dev, v),
+        _ws_at(ws, where, dev), n_ws, _stream(stream))
     if code:
         raise BraError(code, where)
     return dQ, dK, dV
@@ -572,11 +616,14 @@ def norm_workspace(p: BraNormProblem, device="cuda"):
 
 
 def _norm_derived(p):
-    return _tdtype(p), p.B * p.N * p.C, p.C, p.C * (p.B if p.gate == 2 else 1), p.C * (p.B if p.per_image else 1), p.pre != 0
+    # which image a token belongs to matters only where weights are an image's
+    rows = _Shape(p.B, p.N, p.C) if p.gate == 2 or p.per_image else _Shape(p.B * p.N, p.C)
+    return (_tdtype(p), rows, _Shape(p.C), _Shape(p.B, p.C) if p.gate == 2 else _Shape(p.C), _Shape(p.B, p.C) if p.per_image else _Shape(p.C),
+            p.pre != 0)
 
 
-def _weight(t, name, where, numel, dev):
-    return None if t is None else _at(t, name, where, _TORCH.float32, numel, dev)
+def _weight(t, name, where, shape, dev):
+    return None if t is None else _at(t, name, where, _TORCH.float32, shape, dev)
 
 
 def bra_residual_norm(p, x, y=None, gate=None, post_w=None, post_b=None, w=None, b=None, h=None, n=None, stream=None, want_h=True):
@@ -584,22 +631,22 @@ def bra_residual_norm(p, x, y=None, gate=None, post_w=None, post_b=None, w=None,
     if stream is not None and (h is None or n is None):
         with _on(stream):
             return bra_residual_norm(p, x, y, gate, post_w, post_b, w, b, h, n, None, want_h)
-    torch, dev, where = _torch(), _current_device(), "bra_residual_norm"
-    t, size, C, gates, affine, normed = _derived(p, _norm_derived)
-    x_at = _at(x, "x", where, t, size, dev)
-    y_at = None if y is None else _at(y, "y", where, t, size, dev)
+    torch, dev, where = _TORCH or _torch(), (_GET_DEVICE or _device_getter())(), "bra_residual_norm"
+    t, rows, C, gates, affine, normed = _derived(p, _norm_derived)
+    x_at = _at(x, "x", where, t, rows, dev)
+    y_at = None if y is None else _at(y, "y", where, t, rows, dev)
     if h is None and want_h:
         h = torch.empty_like(x)
         h_at = h.data_ptr()
     else:
-        h_at = None if h is None else _at(h, "h", where, t, size, dev)
+        h_at = None if h is None else _at(h, "h", where, t, rows, dev)
     if n is None and normed:
         n = torch.empty_like(x)
         n_at = n.data_ptr()
     else:
-        n_at = None if n is None else _at(n, "n", where, t, size, dev)
+        n_at = None if n is None else _at(n, "n", where, t, rows, dev)
     code = (_LIB or load_library()).bra_residual_norm(
-        ctypes.byref(p), x_at, y_at, _weight(gate, "gate", where, gates, dev), _weight(post_w, "post_w", where, C, dev),
+        byref(p), x_at, y_at, _weight(gate, "gate", where, gates, dev), _weight(post_w, "post_w", where, C, dev),
         _weight(post_b, "post_b", where, C, dev), _weight(w, "w", where, affine, dev), _weight(b, "b", where, affine, dev), h_at, n_at,
         _stream(stream))
     if code:
@@ -613,11 +660,11 @@ def bra_residual_norm_backward(p, x, y, dh, dn, gate=None, post_w=None, post_b=N
     if stream is not None:                                   # the weights' gradients are always its own
         with _on(stream):
             return bra_residual_norm_backward(p, x, y, dh, dn, gate, post_w, post_b, w, b, dx, dy, ws)
-    torch, dev, where = _torch(), _current_device(), "bra_residual_norm_backward"
-    t, size, C, gates, affine, _ = _derived(p, _norm_derived)
-    ins = (_at(x, "x", where, t, size, dev), None if y is None else _at(y, "y", where, t, size, dev), _weight(gate, "gate", where, gates, dev),
+    torch, dev, where = _TORCH or _torch(), (_GET_DEVICE or _device_getter())(), "bra_residual_norm_backward"
+    t, rows, C, gates, affine, _ = _derived(p, _norm_derived)
+    ins = (_at(x, "x", where, t, rows, dev), None if y is None else _at(y, "y", where, t, rows, dev), _weight(gate, "gate", where, gates, dev),
            _weight(post_w, "post_w", where, C, dev), _weight(post_b, "post_b", where, C, dev), _weight(w, "w", where, affine, dev),
-           None if dh is None else _at(dh, "dh", where, t, size, dev), None if dn is None else _at(dn, "dn", where, t, size, dev))
+           None if dh is None else _at(dh, "dh", where, t, rows, dev), None if dn is None else _at(dn, "dn", where, t, rows, dev))
     _weight(b, "b", where, affine, dev)
     if ws is None:
         ws = norm_workspace(p, x.device)
@@ -629,9 +676,9 @@ def bra_residual_norm_backward(p, x, y, dh, dn, gate=None, post_w=None, post_b=N
             out[name] = torch.empty_like(weight)
     n_ws = ws.numel()
     code = (_LIB or load_library()).bra_residual_norm_backward(
-        ctypes.byref(p), *ins, _at(out["dx"], "dx", where, t, size, dev), None if y is None else _at(out["dy"], "dy", where, t, size, dev),
+        byref(p), *ins, _at(out["dx"], "dx", where, t, rows, dev), None if y is None else _at(out["dy"], "dy", where, t, rows, dev),
         *(_ptr(out.get(name)) for name in ("dgate", "d_post_w", "d_post_b", "dw", "db")),
-        _at(ws, "ws", where, torch.uint8, n_ws, dev), n_ws, _stream(stream))
+        _ws_at(ws, where, dev), n_ws, _stream(stream))
     if code:
         raise BraError(code, where)
     return out

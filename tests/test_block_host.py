@@ -313,6 +313,73 @@ def test_what_a_call_makes_belongs_to_its_stream(bra, monkeypatch, handle, as_ob
             assert fake.current == 5
 
 
+# ---------------------------------------------------------------- shapes
+@pytest.fixture
+def host(bra, monkeypatch):
+    """The binding over a library that answers 0 and tensors of the host."""
+    import types
+    import torch
+    from paper_2303_08810_b200 import binding
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *args: 512 if name.endswith("_bytes") else b"refused" if name == "bra_status_string" else 0
+
+    monkeypatch.setattr(binding, "_TORCH", torch)
+    monkeypatch.setattr(binding, "_LIB", Lib())
+    monkeypatch.setattr(binding, "_RAW_STREAM", lambda: 5)
+    monkeypatch.setattr(binding, "_GET_DEVICE", lambda: -1)
+    return types.SimpleNamespace(torch=torch, bra=bra, zeros=lambda *shape, dtype=torch.float32: torch.zeros(*shape, dtype=dtype))
+
+
+@pytest.mark.parametrize("shape,axes,yes", [
+    ((2, 30, 4, 8), (2, 30, 4, 8), True), ((2, 30, 32), (2, 30, 4, 8), True), ((60, 32), (2, 30, 4, 8), True), ((1920,), (2, 30, 4, 8), True),
+    ((2, 5, 6, 32), (2, 30, 4, 8), True), ((2, 1, 5, 6, 2, 2, 8), (2, 30, 4, 8), True), ((60, 4, 2, 4, 1), (2, 30, 4, 8), True),
+    ((2, 960), (2, 30, 4, 8), True), ((2, 4, 30, 8), (2, 30, 4, 8), False), ((30, 2, 32), (2, 30, 4, 8), False),
+    ((2, 30, 8, 4), (2, 30, 4, 8), False), ((4, 2, 30, 8), (2, 30, 4, 8), False), ((2, 32, 30), (2, 30, 4, 8), False),
+    ((20, 96), (2, 30, 4, 8), False), ((2, 30, 31), (2, 30, 4, 8), False), ((7, 3, 1), (3, 7, 1), False), ((3, 7), (3, 7, 1), True),
+    ((2, 30, 32, 2), (2, 30, 4, 8), False), ((0, 32), (2, 30, 4, 8), False), ((), (1, 1), True),
+])
+def test_shapes_that_lay_out_axes(shape, axes, yes):
+    from paper_2303_08810_b200.binding import _lays_out
+    assert _lays_out(shape, axes) is yes
+
+
+def test_calls_refuse_axes_in_another_order(host):
+    """As many elements as the problem has, in another order: refused, with the name of the tensor; nothing of it is remembered."""
+    bra, z, torch = host.bra, host.zeros, host.torch
+    i32, f64 = torch.int32, torch.float64
+    r = bra.make_rope_problem(2, 10, 4, 32, dtype="f32")
+    c = bra.make_cross_problem(2, 10, 12, 4, 32, kv_heads=2, dtype="f32")
+    n = bra.make_norm_problem(2, 10, 64, gate="image", per_image=True, dtype="f32")
+    free = bra.make_norm_problem(2, 10, 64, dtype="f32")
+    q, kv, lse, x = z(2, 10, 4, 32), z(2, 12, 64), z(2, 4, 10), z(2, 10, 64)
+    freq, w = z(16, dtype=f64), z(2, 64)
+    rope = dict(p=r, Q=q, K=q, freq=freq, positions=z(2, 10, dtype=i32))
+    attend = dict(p=c, Q=q, K=kv, V=kv, key_len=z(2, dtype=i32), key_mask=z(2, 12, dtype=torch.bool), lse=lse)
+    back = dict(p=c, Q=q, K=kv, V=kv, O=q, lse=lse, dO=q)
+    norm, norm_back = dict(p=n, x=x, y=x, gate=w, w=w), dict(p=n, x=x, y=x, dh=x, dn=x, gate=w, w=w)
+    heads_first, wrong_kv = z(2, 4, 10, 32), z(2, 2, 12, 32)
+    for call, good, bad in (
+            (bra.bra_rope, rope, dict(Q=heads_first, K=heads_first, Qo=heads_first, Ko=heads_first, positions=z(10, 2, 1, dtype=i32))),
+            (bra.bra_cross_attend, attend, dict(Q=heads_first, K=wrong_kv, V=wrong_kv, O=heads_first, lse=z(2, 10, 4), key_mask=z(12, 2, dtype=torch.bool))),
+            (bra.bra_cross_backward, back, dict(dO=heads_first, O=heads_first, lse=z(10, 2, 4), dQ=heads_first, dK=wrong_kv, dV=wrong_kv)),
+            (bra.bra_residual_norm, norm, dict(x=z(10, 2, 64), y=z(2, 64, 10), gate=z(64, 2), w=z(64, 2), h=z(10, 2, 64), n=z(10, 2, 64))),
+            (bra.bra_residual_norm_backward, norm_back, dict(dh=z(10, 2, 64), dn=z(2, 64, 10), dx=z(10, 2, 64), dy=z(10, 2, 64)))):
+        call(**good)
+        for name, t in bad.items():
+            for _ in range(2):
+                with pytest.raises(bra.BraError, match=f": {name} is") as e:
+                    call(**{**good, name: t})
+                assert e.value.code == SHAPE
+        call(**good)
+    # axes merged and split; without weights of images any order of tokens is one
+    bra.bra_rope(r, z(20, 128), z(2, 2, 5, 128), freq, positions=z(2, 2, 5, 1, dtype=i32))
+    bra.bra_cross_attend(c, z(2, 5, 2, 128), z(24, 64), z(2, 12, 2, 32), key_mask=z(2, 1, 1, 12, dtype=torch.uint8))
+    bra.bra_residual_norm(n, z(2, 2, 5, 64), z(20, 64), gate=z(2, 1, 64), w=z(2, 64))
+    bra.bra_residual_norm(free, z(10, 2, 64))
+
+
 def test_problem_structures_match_the_header(bra):
     """Sizes as a C compiler lays the structures out."""
     import os
