@@ -347,6 +347,7 @@ size_t bra_norm_workspace_bytes(const bra_norm_problem* p);
  *   y     in   [B, N, C], the block's output; NULL: h = alpha * x (the first norm of a network; gate and post must be 0)
  *   gate  in   NULL iff p->gate is BRA_GATE_NONE.   post_w, post_b, w, b  in  each may be NULL (ones, zeros)
  *   h     out  [B, N, C]; may be NULL, may be x or y.   n  out  [B, N, C]; NULL iff p->pre is BRA_NORM_NONE
+ * BRA_ERR_UNSUPPORTED: h shares only a part of its bytes with x or y, or n shares any with x, y or h.
  */
 bra_status bra_residual_norm(const bra_norm_problem* p, const void* x, const void* y, const float* gate,
                              const float* post_w, const float* post_b, const float* w, const float* b,
@@ -356,7 +357,7 @@ bra_status bra_residual_norm(const bra_norm_problem* p, const void* x, const voi
  * Gradients.  dh: of h from what follows in the stream, may be NULL (zeros).  dn: of n, NULL iff p->pre is
  * BRA_NORM_NONE.  dx [B, N, C]; dy [B, N, C], NULL iff y is; the others are fp32 in the shapes of their
  * inputs, each may be NULL where it is not wanted.  The forward pass is made again from x and y, so nothing
- * else has to be kept; the order of every sum is fixed.
+ * else has to be kept; the order of every sum is fixed.  BRA_ERR_UNSUPPORTED: dx or dy shares bytes with x, y, dh, dn or the other.
  */
 bra_status bra_residual_norm_backward(const bra_norm_problem* p, const void* x, const void* y, const float* gate,
                                       const float* post_w, const float* post_b, const float* w,

@@ -853,6 +853,12 @@ Plan plan(const bra_norm_problem* q, bool backward) {
 }
 
 bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+// whether two tensors of [B, N, C] have bytes in common (null: no such tensor)
+bool overlap(const bra_norm_problem* p, const void* a, const void* b) {
+    const uintptr_t u = reinterpret_cast<uintptr_t>(a), v = reinterpret_cast<uintptr_t>(b);
+    const uintptr_t bytes = (uintptr_t)p->B * p->N * p->C * (p->dtype == BRA_BF16 ? 2 : 4);
+    return u && v && (u < v ? v - u : u - v) < bytes;
+}
 
 bra_status check(const bra_norm_problem* p) {
     if (!p) return BRA_ERR_NULL;
@@ -975,7 +981,10 @@ bra_status bra_residual_norm(const bra_norm_problem* p, const void* x, const voi
     if (!y && (p->gate != BRA_GATE_NONE || p->post != BRA_NORM_NONE)) return BRA_ERR_NULL;
     for (const void* q : {x, y, (const void*)h, (const void*)n, (const void*)gate, (const void*)post_w, (const void*)post_b, (const void*)w, (const void*)b})
         if (!aligned_to(q, 16)) return BRA_ERR_ALIGN;
-    if (n == x || n == y || n == h) return BRA_ERR_UNSUPPORTED;
+    // rows are read ahead of the ones written; h may stand in x's or y's very place, where each row is read before it is written
+    for (const void* q : {x, y})
+        if (overlap(p, n, q) || (h != q && overlap(p, h, q))) return BRA_ERR_UNSUPPORTED;
+    if (overlap(p, n, h)) return BRA_ERR_UNSUPPORTED;
     const Plan pl = plan(p, false);
     NormArgs a = args_of(p, pl);
     a.x = x; a.y = y; a.gate = gate; a.post_w = post_w; a.post_b = post_b; a.w = w; a.b = b; a.h = h; a.n = n;
@@ -1001,9 +1010,9 @@ bra_status bra_residual_norm_backward(const bra_norm_problem* p, const void* x, 
     for (const void* q : {x, y, dh, dn, (const void*)dx, (const void*)dy, (const void*)gate, (const void*)post_w, (const void*)post_b,
                           (const void*)w, (const void*)d_gate, (const void*)d_post_w, (const void*)d_post_b, (const void*)d_w, (const void*)d_b})
         if (!aligned_to(q, 16)) return BRA_ERR_ALIGN;
-    if (dx == dy) return BRA_ERR_UNSUPPORTED;
+    if (overlap(p, dx, dy)) return BRA_ERR_UNSUPPORTED;
     for (const void* q : {x, y, dh, dn})
-        if (q && (q == dx || q == dy)) return BRA_ERR_UNSUPPORTED;      // rows are read ahead of the ones written
+        if (overlap(p, q, dx) || overlap(p, q, dy)) return BRA_ERR_UNSUPPORTED;      // rows are read ahead of the ones written
     if (!ws) return BRA_ERR_NULL;
     if (!aligned_to(ws, 256)) return BRA_ERR_ALIGN;
     if (ws_bytes < bra_norm_workspace_bytes(p)) return BRA_ERR_WORKSPACE;

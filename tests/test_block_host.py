@@ -182,6 +182,27 @@ def test_norm_refuses_bad_pointers(bra):
     assert norm(bra, back=True, ws_bytes=need - 1) == WORKSPACE
 
 
+def test_norm_refuses_outputs_that_overlap(bra):
+    """Any bytes in common, not only the same address: rows are read ahead of the ones written."""
+    B = A + (1 << 20)
+    size = 2 * 5 * 64 * 2                                            # of a tensor in bytes
+    for off in (16, size // 2, size - 16):
+        for n in (A - off, A + off, B - off, B + off):               # n over x (and y) or h
+            assert norm(bra, n=n) == UNSUPPORTED
+        for h in (A - off, A + off):
+            assert norm(bra, h=h, n=8 * B) == UNSUPPORTED
+            assert norm(bra, h=h, x=32 * B, n=8 * B) == UNSUPPORTED
+        for at in (A - off, A + off):                                # dx or dy over x, y, dh, dn
+            for first in (dict(x=at), dict(y=at), dict(dh=at), dict(dn=at)):
+                for out in ("dx", "dy"):
+                    far = dict(x=32 * B, y=32 * B, dh=32 * B, dn=32 * B, dx=64 * B, dy=128 * B)
+                    assert norm(bra, back=True, **{**far, **first, out: A}) == UNSUPPORTED
+        assert norm(bra, back=True, dx=64 * B, dy=64 * B + off) == UNSUPPORTED
+    # next to one another is apart: refused for want of scratch only
+    apart = dict(x=64 * B, y=64 * B + size, dh=64 * B + 2 * size, dn=64 * B + 3 * size, dx=64 * B + 4 * size, dy=64 * B + 5 * size)
+    assert norm(bra, back=True, ws=None, **apart) == NULL
+
+
 COLUMNS = r"""
 #include <stdio.h>
 #include <vector>
