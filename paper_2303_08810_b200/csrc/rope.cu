@@ -139,13 +139,15 @@ __global__ void __launch_bounds__(ROPE_THREADS, ROPE_CTAS<T, VEC, HALF>) rope_ke
             if (e < turned) {
                 const int ax = HALF ? axis : (pair + e >= half ? 1 : 0);
                 // Turns per position as a fraction of 2^64: coordinate * that, modulo 2^64, is the angle without its whole turns, exactly.
+                // (An infinite or NaN frequency leaves t NaN, which no integer can say.)
                 double t = __ldg(g.freq + (pair + e - ax * half)) * 0.15915494309189533577;
                 t -= floor(t);
                 const unsigned long long step = t < 1.0 ? __double2ull_rn(t * 18446744073709551616.0) : 0ull;
                 const unsigned long long angle = (unsigned long long)(long long)(ax ? place[1] : place[0]) * step;
                 float sn, cn;
                 sincospif((float)(int)(angle >> 32) * 4.656612873077392578125e-10f, &sn, &cn);      // 2^-31 half turns, in [-1, 1)
-                cs[e] = make_float2(cn * g.magnitude, sn * g.magnitude * g.sine);
+                const float nan = __int_as_float(0x7fffffff);
+                cs[e] = t == t ? make_float2(cn * g.magnitude, sn * g.magnitude * g.sine) : make_float2(nan, nan);
             }
         }
     }

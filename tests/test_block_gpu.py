@@ -729,6 +729,29 @@ def test_norm_over_its_input(bra, C, dtype, onto):
     assert all(torch.equal(t[N * C:], u) for t, u in zip(full, tail))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["interleaved", "half"])
+@pytest.mark.parametrize("D", [6, 32])
+def test_rope_frequencies_that_are_no_numbers(bra, D, layout, dtype):
+    """A pair whose frequency is NaN or infinite has no angle: it comes out NaN (at coordinate 0 too), the others as they were."""
+    import torch
+    x = randn(40, 2, 5, 3 * D, dtype=dtype)
+    p = bra.make_rope_problem(2, 5, 3, D, kv_heads=0, layout=layout, dtype=dtype)
+    good = bra.rope_frequencies(D)
+    want = bra.bra_rope(p, x, None, good)[0].view(2, 5, 3, D)
+    for value in (math.nan, math.inf, -math.inf):
+        for pair in (0, D // 2 - 1):
+            freq = good.clone()
+            freq[pair] = value
+            mine = torch.zeros(D, dtype=torch.bool, device="cuda")
+            mine[[2 * pair, 2 * pair + 1] if layout == "interleaved" else [pair, pair + D // 2]] = True
+            for inverse in (False, True):
+                got = bra.bra_rope(p, x, None, freq, inverse=inverse)[0].view(2, 5, 3, D)
+                assert bool(torch.isnan(got[..., mine]).all())
+                if not inverse:
+                    assert torch.equal(got[..., ~mine], want[..., ~mine])
+
+
 # ---------------------------------------------------------------- another stream
 def test_calls_on_a_stream_while_the_current_one_is_busy(bra):
     """Outputs and scratch that the calls make themselves, on a stream given as an object and as a handle, behind nothing of the current
