@@ -18,10 +18,13 @@ namespace bra {
 namespace {
 
 constexpr int THREADS = 128, KEPT = 64;
+// Walked rows of a tile, and the step by which walks are cut: a part's length is a multiple of it, so only the end of the rows (or keys)
+// cuts a tile.
+constexpr int walk_tile(int D) { return D == 128 ? 32 : 64; }
 
 template <int D, bool DKV>
 struct Shape {
-    static constexpr int BN = D == 128 ? 32 : 64;           // walked rows of a tile
+    static constexpr int BN = walk_tile(D);
     static constexpr int TILE = BN * D * 2;
     static constexpr bool X_SHARED = D == 128;              // X fragments are read from shared memory for every tile
     static constexpr int STATS = DKV ? BN * 8 : 0;          // (lse2, delta) of the walked rows
@@ -29,6 +32,7 @@ struct Shape {
     static constexpr int X = X_SHARED ? 2 * KEPT * D * 2 : 0;
     static constexpr size_t smem = 2 * STAGE + X;
     static constexpr int SUMS = DKV ? 2 : 1;
+    static_assert(KEPT % BN == 0, "the statistics of a walk's last tile");
 };
 
 template <int D, bool DKV>
@@ -140,8 +144,8 @@ __global__ void __launch_bounds__(THREADS) cross_grad_kernel(const CrossArgs a) 
                 ptx::cp_async_16(to + S::TILE, V + jj * a.v_stride + ch * 8, have ? 16 : 0);
             }
         }
-        // statistics exist up to the padded number of rows; a tile that is cut by the end of a split reads rows of the next,
-        // whose Q and dO are zeros here
+        // statistics exist up to the padded number of rows (a multiple of BN); rows that do not exist have (inf, 0), so their P and dS are
+        // zero whatever their scores
         if (DKV && threadIdx.x < BN / 2)
             ptx::cp_async_16(to0 + 2 * S::TILE + threadIdx.x * 16, stats + walk_lo + tile * BN + threadIdx.x * 2, 16);
     };
@@ -289,8 +293,7 @@ __global__ void __launch_bounds__(THREADS) cross_grad_kernel(const CrossArgs a) 
 }
 
 CrossSplit split_of(const CrossDims& d, bool dkv) {
-    const int step = d.D == 128 ? 32 : 64;
-    return cross_split((long long)d.B * d.kv, dkv ? d.Nk : d.rows, KEPT, dkv ? d.rows : d.Nk, step, 2);
+    return cross_split((long long)d.B * d.kv, dkv ? d.Nk : d.rows, KEPT, dkv ? d.rows : d.Nk, walk_tile(d.D), 2);
 }
 
 template <int D, bool DKV>

@@ -26,13 +26,16 @@ namespace bra {
 namespace {
 
 constexpr int THREADS = 128, KEPT = 64;
+// Walked rows of a tile, and the step by which walks are cut: a part's length is a multiple of it, so only the end of the rows (or keys)
+// cuts a tile.
+constexpr int walk_tile(int D) { return D == 128 ? 32 : 64; }
 
 template <int D>
 struct Shape {
     static constexpr int GW = D < 32 ? D : 32, NG = D / GW;     // channels of a group, groups
     static constexpr int LC = GW / 4;                           // neighbouring channels of a lane, contracted over
     static constexpr int NB = GW / 8;                           // column blocks of a group, columns of a lane
-    static constexpr int BN = D == 128 ? 32 : 64;               // walked rows of a tile
+    static constexpr int BN = walk_tile(D);
     static constexpr int LD = (D + 4) * 4;                      // bytes of a row in shared memory
     static constexpr int TILE = BN * LD;
 };
@@ -390,7 +393,8 @@ __global__ void __launch_bounds__(THREADS, D == 128 ? 1 : 2) cross_grad_tf32_ker
     const float *Q = static_cast<const float*>(a.Q), *dO = static_cast<const float*>(a.dO);
     const float* K = static_cast<const float*>(a.K) + (long long)at.b * a.Nk * a.k_stride + (long long)at.kvh * D;
     const float* V = static_cast<const float*>(a.V) + (long long)at.b * a.Nk * a.v_stride + (long long)at.kvh * D;
-    const int padded = (a.rows + 63) / 64 * 64;
+    static_assert(KEPT % S::BN == 0, "the statistics of a walk's last tile");
+    const int padded = (a.rows + KEPT - 1) / KEPT * KEPT;
     float2* stats = a.stats + at.pair * padded;             // log of the softmax denominator, delta
     const uint32_t base = ptx::smem_u32(sh);
     int tiles = walk_hi > walk_lo ? (walk_hi - walk_lo + S::BN - 1) / S::BN : 0;
@@ -408,7 +412,8 @@ __global__ void __launch_bounds__(THREADS, D == 128 ? 1 : 2) cross_grad_tf32_ker
             o2 = j * a.v_stride;
             return (keys.word(tile * (S::BN / 32) + (row >> 5)) >> (row & 31)) & 1;
         });
-        // (a tile that is cut by the end of a part reads the statistics of rows of the next, whose Q and dO are zeros here)
+        // statistics exist up to the padded number of rows (a multiple of BN); rows that do not exist have (inf, 0), so their P and dS are
+        // zero whatever their scores
         if (DKV && threadIdx.x < S::BN / 2)
             ptx::cp_async_16(base + stage * STAGE + 2 * S::TILE + threadIdx.x * 16, stats + walk_lo + tile * S::BN + threadIdx.x * 2, 16);
         ptx::cp_async_commit();
@@ -556,11 +561,10 @@ __global__ void __launch_bounds__(THREADS, D == 128 ? 1 : 2) cross_grad_tf32_ker
 
 // ---------------------------------------------------------------- host
 bool few_rows(const CrossDims& d) { return d.rows <= 16; }
-int step(const CrossDims& d) { return d.D == 128 ? 32 : 64; }
 
-CrossSplit forward_split(const CrossDims& d) { return cross_split((long long)d.B * d.kv, d.rows, few_rows(d) ? 16 : KEPT, d.Nk, step(d), 3); }
+CrossSplit forward_split(const CrossDims& d) { return cross_split((long long)d.B * d.kv, d.rows, few_rows(d) ? 16 : KEPT, d.Nk, walk_tile(d.D), 3); }
 CrossSplit grad_split(const CrossDims& d, bool dkv) {
-    return cross_split((long long)d.B * d.kv, dkv ? d.Nk : d.rows, KEPT, dkv ? d.rows : d.Nk, step(d), 2);
+    return cross_split((long long)d.B * d.kv, dkv ? d.Nk : d.rows, KEPT, dkv ? d.rows : d.Nk, walk_tile(d.D), 2);
 }
 
 template <typename Kernel>
