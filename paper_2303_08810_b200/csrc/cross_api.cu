@@ -12,7 +12,7 @@ CrossSplit cross_split(long long pairs, long long rows, int tile_rows, int summe
     const int steps = (summed + step - 1) / step;
     const long long out = pairs * s.tiles;
     // fewer output tiles than SMs, and more than two steps of the walk for each part
-    if (out < kSMs && out <= CROSS_COUNTERS) {
+    if (out < kSMs) {
         const long long want = (long long)kSMs * per_sm / out, most = steps / 2;
         s.splits = (int)(want < most ? want : most);
         if (s.splits < 1) s.splits = 1;

@@ -13,6 +13,7 @@
 namespace bra {
 
 constexpr int CROSS_COUNTERS = 2048;                // parts of split sums that are done, one counter per output tile
+static_assert(kSMs <= CROSS_COUNTERS, "walks are split where output tiles are fewer than SMs");
 constexpr int CROSS_MASKED_KEYS = 1 << 19;          // most keys of an image with a key mask: their bits are held in shared memory
 
 struct CrossDims {

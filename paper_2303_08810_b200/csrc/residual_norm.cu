@@ -29,7 +29,6 @@ struct NormArgs {
     long long rows;
     int N;                                  // rows of an image
     int C;
-    int group;                              // threads of a row
     int run;                                // rows of a CTA
     int gate_image, affine_image;           // [B, C] rather than [C]
     int pre, post;
@@ -757,7 +756,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 384 || (THREADS == 128 && 
 struct JoinArgs {
     const float* part;
     float* out[SUMS];
-    long long slots, rows;
+    long long slots;
     int N, C, run, ctas, images;
     int image_sum[SUMS];                    // [B, C] rather than [C]
     int which[SUMS];
@@ -876,7 +875,7 @@ bra_status check(const bra_norm_problem* p) {
 NormArgs args_of(const bra_norm_problem* p, const Plan& pl) {
     NormArgs a = {};
     a.rows = (long long)p->B * p->N;
-    a.N = p->N; a.C = p->C; a.group = pl.group; a.run = pl.run;
+    a.N = p->N; a.C = p->C; a.run = pl.run;
     a.gate_image = p->gate == BRA_GATE_IMAGE; a.affine_image = p->per_image != 0;
     a.pre = p->pre; a.post = p->post; a.eps = p->eps; a.alpha = p->alpha;
     return a;
@@ -1022,7 +1021,7 @@ bra_status bra_residual_norm_backward(const bra_norm_problem* p, const void* x, 
     a.part = static_cast<float*>(ws);
     a.slots = slots_of(p, pl);
     JoinArgs j = {};
-    j.part = a.part; j.slots = a.slots; j.rows = a.rows; j.N = p->N; j.C = p->C; j.run = pl.run; j.ctas = (int)pl.ctas; j.images = p->B;
+    j.part = a.part; j.slots = a.slots; j.N = p->N; j.C = p->C; j.run = pl.run; j.ctas = (int)pl.ctas; j.images = p->B;
     float* outs[SUMS] = {d_w, d_b, d_gate, d_post_w, d_post_b};
     const int of_image[SUMS] = {a.affine_image, a.affine_image, a.gate_image, 0, 0};
     int wanted = 0, most_images = 1;
