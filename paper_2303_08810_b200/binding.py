@@ -241,7 +241,7 @@ def _check(code, where):
 
 def bra_route(p, Q, K, q_mean=None, k_mean=None, index=None, ws=None, stream=None, want_means=True):
     """bra_route: Q, K -> (q_mean, k_mean, index)."""
-    if stream is not None and (ws is None or index is None or q_mean is None or k_mean is None):
+    if stream is not None and (ws is None or index is None or (want_means and (q_mean is None or k_mean is None))):
         with _on(stream):
             return bra_route(p, Q, K, q_mean, k_mean, index, ws, None, want_means)
     torch = _torch()
@@ -284,7 +284,7 @@ def bra_route_static(p, Q, K, index=None, stream=None):
 def bra_attend(p, Q, K, V, index, lce_w=None, lce_b=None, O=None, lse=None, ws=None, stream=None,
                want_lse=True):
     """bra_attend: Q, K, V, index -> (O, lse)."""
-    if stream is not None and (ws is None or O is None or lse is None):
+    if stream is not None and (ws is None or O is None or (lse is None and want_lse)):
         with _on(stream):
             return bra_attend(p, Q, K, V, index, lce_w, lce_b, O, lse, ws, None, want_lse)
     torch = _torch()
@@ -302,7 +302,7 @@ def bra_attend(p, Q, K, V, index, lce_w=None, lce_b=None, O=None, lse=None, ws=N
 def bra_forward(p, Q, K, V, lce_w=None, lce_b=None, O=None, index=None, lse=None, ws=None,
                 stream=None, want_index=True, want_lse=True):
     """bra_forward: Q, K, V -> (O, index, lse)."""
-    if stream is not None and (ws is None or O is None or index is None or lse is None):
+    if stream is not None and (ws is None or O is None or (index is None and want_index) or (lse is None and want_lse)):
         with _on(stream):
             return bra_forward(p, Q, K, V, lce_w, lce_b, O, index, lse, ws, None, want_index, want_lse)
     torch = _torch()
@@ -322,7 +322,8 @@ def bra_forward(p, Q, K, V, lce_w=None, lce_b=None, O=None, index=None, lse=None
 def bra_backward(p, Q, K, V, index, lce_w, lse, dO, dQ=None, dK=None, dV=None, d_lce_w=None,
                  d_lce_b=None, ws=None, stream=None, want_bias_grad=False):
     """bra_backward: -> (dQ, dK, dV, d_lce_w, d_lce_b)."""
-    if stream is not None and any(t is None for t in (ws, dQ, dK, dV, d_lce_w, d_lce_b)):
+    if stream is not None and (ws is None or dQ is None or dK is None or dV is None or (d_lce_w is None and p.lce_ksize) or
+                               (d_lce_b is None and want_bias_grad)):
         with _on(stream):
             return bra_backward(p, Q, K, V, index, lce_w, lse, dO, dQ, dK, dV, d_lce_w, d_lce_b, ws, None, want_bias_grad)
     torch = _torch()
@@ -492,7 +493,7 @@ def _rope_derived(p):
 
 def bra_rope(p, Q, K, freq, positions=None, Qo=None, Ko=None, inverse=False, stream=None):
     """bra_rope: Q, K -> (Qo, Ko).  Pass Q and K as Qo and Ko to rotate in place; inverse=True is the gradient's rotation."""
-    if stream is not None and (Qo is None or Ko is None):
+    if stream is not None and (Qo is None or (Ko is None and K is not None)):
         with _on(stream):
             return bra_rope(p, Q, K, freq, positions, Qo, Ko, inverse)
     torch, dev, where = _TORCH or _torch(), (_GET_DEVICE or _device_getter())(), "bra_rope"
@@ -549,7 +550,7 @@ def _cross_mask(key_len, key_mask, where, torch, images, keys, dev):
 
 def bra_cross_attend(p, Q, K, V, key_len=None, key_mask=None, O=None, lse=None, ws=None, stream=None, want_lse=True):
     """bra_cross_attend: Q, K, V -> (O, lse).  key_len int32 [B], key_mask bool or uint8 [B, Nk]."""
-    if stream is not None and (ws is None or O is None or lse is None):
+    if stream is not None and (ws is None or O is None or (lse is None and want_lse)):
         with _on(stream):
             return bra_cross_attend(p, Q, K, V, key_len, key_mask, O, lse, ws, None, want_lse)
     torch, dev, where = _TORCH or _torch(), (_GET_DEVICE or _device_getter())(), "bra_cross_attend"
@@ -628,7 +629,7 @@ def _weight(t, name, where, shape, dev):
 
 def bra_residual_norm(p, x, y=None, gate=None, post_w=None, post_b=None, w=None, b=None, h=None, n=None, stream=None, want_h=True):
     """bra_residual_norm: x, y -> (h, n): the residual stream behind the block, and what the next block reads."""
-    if stream is not None and (h is None or n is None):
+    if stream is not None and ((h is None and want_h) or (n is None and p.pre)):
         with _on(stream):
             return bra_residual_norm(p, x, y, gate, post_w, post_b, w, b, h, n, None, want_h)
     torch, dev, where = _TORCH or _torch(), (_GET_DEVICE or _device_getter())(), "bra_residual_norm"

@@ -334,6 +334,28 @@ def test_what_a_call_makes_belongs_to_its_stream(bra, monkeypatch, handle, as_ob
             assert fake.current == 5
 
 
+def test_a_call_that_makes_nothing_leaves_the_current_stream(host, monkeypatch):
+    """With all outputs and scratch given, and what is not wanted left out, a stream is only passed on."""
+    from paper_2303_08810_b200 import binding
+    bra, z, torch = host.bra, host.zeros, host.torch
+    monkeypatch.setattr(binding, "_on", lambda stream: pytest.fail("entered"))
+    p = bra.make_problem(1, 8, 8, 64, heads=2, S=2, topk=1, dtype="f32", lce=False)
+    m, idx, ws, lse = z(1, 8, 8, 64), z(1, 2, 4, 1, dtype=torch.int32), z(512, dtype=torch.uint8), z(1, 2, 64)
+    r = bra.make_rope_problem(1, 64, 2, 32, kv_heads=0, dtype="f32")
+    c = bra.make_cross_problem(1, 64, 64, 2, 32, dtype="f32")
+    n = bra.make_norm_problem(1, 64, 64, pre="none", dtype="f32")
+    t = z(1, 64, 64)
+    bra.bra_route(p, m, m, index=idx, ws=ws, want_means=False, stream=7)
+    bra.bra_route_static(p, m, m, index=idx, stream=7)
+    bra.bra_attend(p, m, m, m, idx, O=m, ws=ws, want_lse=False, stream=7)
+    bra.bra_forward(p, m, m, m, O=m, ws=ws, want_index=False, want_lse=False, stream=7)
+    bra.bra_backward(p, m, m, m, idx, None, lse, m, dQ=m, dK=m, dV=m, ws=ws, stream=7)
+    bra.bra_rope(r, t, None, z(16, dtype=torch.float64), Qo=t, stream=7)
+    bra.bra_cross_attend(c, t, t, t, O=t, ws=ws, want_lse=False, stream=7)
+    bra.bra_cross_backward(c, t, t, t, t, lse, t, dQ=t, dK=t, dV=t, ws=ws, stream=7)
+    bra.bra_residual_norm(n, t, t, h=t, stream=7)
+
+
 # ---------------------------------------------------------------- shapes
 @pytest.fixture
 def host(bra, monkeypatch):
