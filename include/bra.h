@@ -266,7 +266,7 @@ bra_status bra_rope_frequencies(int32_t rot_dim, int32_t axes, double base, int3
 /*
  * Rotates Q and K (K NULL iff kv_heads is 0) in one launch.
  *   positions in   int32 [B, N, axes], or NULL: those that the problem implies
- *   freq      in   double [rot_dim / axes / 2], on the device
+ *   freq      in   double [rot_dim / axes / 2], on the device; a pair whose frequency is infinite or NaN comes out NaN
  *   inverse   in   nonzero: by the negative angle.  That is the transpose, so it is also the gradient:
  *                  dQ = bra_rope(inverse) of the gradient of Qo.
  *   Qo, Ko    out  laid out like Q, K; each may be the very same tensor (in place)

@@ -2,7 +2,8 @@
 //
 // A pair of channels (u, v) of a token turns by the angle coordinate * freq, the same for every head of Q and K.  The angle is
 // formed in 64 bits (at coordinate 10^6 a 32-bit product is off by 0.03 radians), and only what is left of it without whole turns
-// goes to 32 bits.
+// goes to 32 bits and a float: half a step of an angle below half a turn is 9.4 10^-8 radians, of the order of the fp32 outputs' own rounding
+// (their error against 64 bits 3.9 10^-8; of a plain form with angles in 64 bits 3.0 10^-8).
 //
 // What bounds it: HBM, every channel read and written once.  A thread has 16 bytes of a head (half layout: and the 16 that belong to
 // them) of one token, makes the (cos, sin) of its pairs once, in registers, and walks the heads of Q and K with them - of all images,
